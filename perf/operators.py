@@ -189,7 +189,7 @@ def _inputs(c, seed):
         s["weight"] = torch.where(valid, scale * t * t / valid.sum(), 0.0).float()
         if c["kind"] == "backward":
             s["upstream"] = torch.rand(rows, generator=gen, device="cuda") + 0.5
-            s["stats"] = _stats(s)
+            s["stats"] = _saved(s)
         return s
     z = _matrix(c, gen, 1.0)
     noisy = z.float() + 0.5 * torch.randn(cols, generator=gen, device="cuda")
@@ -298,21 +298,35 @@ def _spread(c, place, value, like):
     return out.scatter_(1, place, value)[:, :-1]
 
 
-def _stats(s):
-    """What the forward pass saves per row: the largest logit, 1 / sum of exponentials, 1 - p_rest / q_rest, and the
-    teacher's largest entry and 1 / sum of exponentials."""
-    c = s["case"]
-    place, _, p_rest, m_t, n_t = _teacher(s)
+def _student(s, place, p_rest):
+    """(the exponentials of the row's logits less the largest one, their sum, the sum over the columns not kept, the
+    largest logit, the largest one not kept, what a column not kept has for a gradient per exp((z - that) / t))"""
+    t = s["case"]["temperature"]
     z = s["logits"].float()
+    kept = _spread(s["case"], place, torch.ones_like(place, dtype=torch.bool), torch.bool)
     m = z.max(1).values
-    e = torch.exp((z - m[:, None]) / c["temperature"])
+    e = torch.exp((z - m[:, None]) / t)
     n = e.sum(1)
-    kept = _spread(c, place, torch.ones_like(place, dtype=torch.bool), torch.bool)
-    tail = torch.where(kept, 0.0, e).sum(1)
-    stats = torch.zeros(c["rows"], STATS, device="cuda")
-    for i, x in enumerate((m, 1.0 / n, 1.0 - p_rest * (n / tail), m_t, 1.0 / n_t)):
+    others = torch.where(kept, float("-inf"), z)
+    m_tail = others.max(1).values
+    tail = torch.exp((others - m_tail[:, None]) / t).sum(1)
+    factor = torch.exp((m_tail - m) / t) / n - p_rest / tail
+    return kept, m, n, m_tail, tail, factor
+
+
+def _stats(s, m, n, m_tail, factor, m_t, n_t):
+    """What the forward pass saves per row."""
+    stats = torch.zeros(s["case"]["rows"], STATS, device="cuda")
+    for i, x in enumerate((m, 1.0 / n, m_tail, factor, m_t, 1.0 / n_t)):
         stats[:, i] = torch.where(s["weight"] == 0, 0.0, x)
     return stats
+
+
+def _saved(s):
+    """The saved numbers of a backward pass that is measured by itself."""
+    place, _, p_rest, m_t, n_t = _teacher(s)
+    _, m, n, m_tail, _, factor = _student(s, place, p_rest)
+    return _stats(s, m, n, m_tail, factor, m_t, n_t)
 
 
 def _run_plain(s):
@@ -359,37 +373,31 @@ def _plain_top(s):
 
 def _plain_distill(s):
     c = s["case"]
-    t = c["temperature"]
+    t, w = c["temperature"], s["weight"]
     out = {}
     place, p, p_rest, m_t, n_t = _teacher(s)
     z = s["logits"].float()
-    kept = _spread(c, place, torch.ones_like(place, dtype=torch.bool), torch.bool)
-    w = s["weight"]
     if c["kind"] == "backward":
-        st = s["stats"]
-        q = torch.exp((z - st[:, :1]) / t) * st[:, 1:2]
-        factor, w = st[:, 2], w * s["upstream"]
+        m, inv_n, m_tail, factor = (s["stats"][:, i] for i in range(4))
+        kept = _spread(c, place, torch.ones_like(place, dtype=torch.bool), torch.bool)
+        w = w * s["upstream"]
     else:
-        m = z.max(1).values
-        e = torch.exp((z - m[:, None]) / t)
-        n = e.sum(1)
-        tail = torch.where(kept, 0.0, e).sum(1)
-        q = e / n[:, None]
-        factor = 1.0 - p_rest * (n / tail)
+        kept, m, n, m_tail, tail, factor = _student(s, place, p_rest)
+        inv_n = 1.0 / n
         there = place < c["cols"]
         zk = torch.gather(z, 1, torch.where(there, place, 0))
-        log_q = (zk - m[:, None]) / t - torch.log(n)[:, None]
-        log_p = torch.where(there, s["val"].float() / t, float("-inf")) - (m_t + torch.log(n_t))[:, None]
+        log_n, log_t = torch.log(n), m_t + torch.log(n_t)
+        log_q = (zk - m[:, None]) / t - log_n[:, None]
+        log_p = torch.where(there, s["val"].float() / t, float("-inf")) - log_t[:, None]
         terms = torch.where(p > 0, p * (log_p - log_q), 0.0).sum(1)
-        last = p_rest * ((s["rest"] - m_t - torch.log(n_t)) - (torch.log(tail) - torch.log(n)))
+        last = p_rest * (s["rest"] - log_t - (torch.log(tail) + (m_tail - m) / t - log_n))
         out["loss"] = torch.where(w == 0, 0.0, w * (terms + torch.where(p_rest > 0, last, 0.0)))
     if c["kind"] == "forward":
-        stats = torch.zeros(c["rows"], STATS, device="cuda")
-        for i, x in enumerate((m, 1.0 / n, factor, m_t, 1.0 / n_t)):
-            stats[:, i] = torch.where(w == 0, 0.0, x)
-        out["stats"] = stats
+        out["stats"] = _stats(s, m, n, m_tail, factor, m_t, n_t)
         return out
-    g = torch.where(kept, q - _spread(c, place, p, torch.float32), q * factor[:, None]) * (w / t)[:, None]
+    q = torch.exp((z - m[:, None]) / t) * inv_n[:, None] - _spread(c, place, p, torch.float32)
+    others = torch.exp((z - m_tail[:, None]) / t) * factor[:, None]
+    g = torch.where(kept, q, others) * (w / t)[:, None]
     out["grad"] = torch.where((w == 0)[:, None], 0.0, g).to(DTYPE[c["type"]])
     return out
 
@@ -498,7 +506,10 @@ def _exact_distill(s, part):
     if c["kind"] == "forward":
         m, m_t = z.max(1).values, torch.maximum(entry.max(1).values, s["rest"][part].double())
         log_sum = torch.logsumexp(torch.cat([entry, s["rest"][part].double()[:, None]], 1), 1)
-        cols = [m * t, torch.exp(m - torch.logsumexp(z, 1)), factor, m_t, torch.exp(m_t - log_sum)]
+        m_tail = torch.where(kept, float("-inf"), z).max(1).values
+        tail = torch.exp(torch.where(kept, float("-inf"), z) - m_tail[:, None]).sum(1)
+        cols = [m * t, torch.exp(m - torch.logsumexp(z, 1)), m_tail * t, (torch.exp(log_tail) - p_rest) / tail, m_t,
+                torch.exp(m_t - log_sum)]
         stats = torch.stack(cols + [torch.zeros_like(m)] * (STATS - len(cols)), 1)
         out["stats"] = torch.where(live[:, None], stats, 0.0)
         return out
