@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdeepreduce.so")
 ARCH = os.environ.get("DR_OFFLOAD_ARCH", "gfx950")
 
-SOURCES = ["select.hip", "bloom.hip", "valuefit.hip", "api.hip"]
+SOURCES = ["select.hip", "bloom.hip", "valuefit.hip", "api.hip", "toplogits.hip", "distill.hip", "balance.hip",
+           "losses_api.hip"]
 
 COMMON = [
     "-O3",

@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "deepreduce.h"
+#include "host.hpp"
 #include "launch.hpp"
 
 using namespace dr;
@@ -29,11 +30,10 @@ static_assert(LAYOUT_STANDARD == DR_FILTER_STANDARD && LAYOUT_PARTITIONED == DR_
 static_assert(MAX_SEG == DR_MAX_SEGMENTS && MAX_DEG == DR_MAX_DEGREE, "limits of the header and the kernels");
 
 namespace {
-
 thread_local std::string g_err;
+}  // namespace
 
-void trace_call(hipStream_t s);  // per-kernel timing, defined below
-
+namespace dr {
 dr_status fail(dr_status st, const char *fmt, ...) {
     char buf[512];
     va_list ap;
@@ -48,14 +48,12 @@ dr_status hip_fail(hipError_t e, const char *where) {
     return fail(DR_EDEVICE, "%s: %s", where, hipGetErrorString(e));
 }
 
-#define DR_HIP(call)                                       \
-    do {                                                   \
-        hipError_t e_ = (call);                            \
-        if (e_ != hipSuccess) return hip_fail(e_, #call);  \
-    } while (0)
+bool ws_ok(const void *ws, size_t ws_bytes, size_t need) {
+    return ws && ws_bytes >= need && ((uintptr_t)ws & 255u) == 0;
+}
+}  // namespace dr
 
-uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
-uint64_t align_up(uint64_t a, uint64_t b) { return ceil_div(a, b) * b; }
+namespace {
 
 // Remark 2 of Section 10.2, rounded (see deepreduce.h)
 bool bloom_params_host(uint64_t n, double fpr, uint64_t *m, uint32_t *k) {
@@ -811,10 +809,6 @@ TInit receiver_init(const TInit &in) {
     return r;
 }
 
-bool ws_ok(void *ws, size_t ws_bytes, size_t need) {
-    return ws && ws_bytes >= need && ((uintptr_t)ws & 255u) == 0;
-}
-
 // The sender in two halves: select, insert, query and the values' layout
 // (front), then sort, segmentation, fit and reorder map (back).
 struct Encode {
@@ -1440,13 +1434,12 @@ void trace_record(hipStream_t s, const char *name) {
     g_trace.marks.push_back({name, ev, s});
 }
 
-// every entry point that launches work marks its start
-void trace_call(hipStream_t s) { trace_record(s, nullptr); }
-
-
 }  // namespace
 
 namespace dr {
+// every entry point that launches work marks its start
+void trace_call(hipStream_t s) { trace_record(s, nullptr); }
+
 // Compute units of the current device (cached per device).
 int device_cus() {
     static int cus[64] = {0};

@@ -1,0 +1,314 @@
+// losses.hpp -- what the loss kernels share: number types and their 16-byte
+// vectors, row slices, block reductions, and the host-side launchers.
+//
+// A row of logits is cut into slices, one block each: a slice is held in
+// registers from one read, so that its maximum and its sum of exponentials
+// take one pass over memory, and rows that are few still fill the chip.  The
+// slices' results are joined in a second, small launch.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <stdint.h>
+
+#include "dr_common.hpp"
+
+namespace dr {
+
+constexpr uint32_t TYPE_F32 = 0, TYPE_BF16 = 1, TYPE_F16 = 2;
+constexpr uint32_t INDEX_I32 = 0, INDEX_I64 = 1;
+constexpr uint32_t MAX_TOP = 256, MAX_TEACHER = 1024, MAX_EXPERTS = 1024;
+constexpr uint32_t STATS = 8;  // floats saved per row by the distillation's forward pass
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float F_LOWEST = -3.4028234663852886e38f;
+constexpr float F_NEG_INF = -__builtin_inff();
+constexpr uint32_t KEY_NEG_INF = 0x007fffffu;  // order_key(-inf)
+
+inline uint32_t type_bytes(uint32_t type) { return type == TYPE_F32 ? 4u : 2u; }
+
+// A matrix of logits (or of gradients) as the kernels take it.
+struct Matrix {
+    const void *p;
+    uint64_t rows, stride;
+    uint32_t cols;
+    uint32_t type;
+};
+
+// A number type: its storage, and how many a 16-byte vector holds.
+template <uint32_t TYPE>
+struct Num {
+    using T = uint16_t;
+    static constexpr uint32_t VEC = 8;
+    static constexpr uint32_t NEG_INF = TYPE == TYPE_BF16 ? 0xff80u : 0xfc00u;
+};
+template <>
+struct Num<TYPE_F32> {
+    using T = uint32_t;
+    static constexpr uint32_t VEC = 4;
+    static constexpr uint32_t NEG_INF = 0xff800000u;
+};
+
+#if defined(__HIPCC__)
+
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf162_t __attribute__((ext_vector_type(2)));
+typedef float float2_t __attribute__((ext_vector_type(2)));
+
+template <uint32_t TYPE>
+__device__ __forceinline__ float num_float(typename Num<TYPE>::T x) {
+    if constexpr (TYPE == TYPE_F32)
+        return __uint_as_float(x);
+    else if constexpr (TYPE == TYPE_BF16)
+        return __uint_as_float((uint32_t)x << 16);
+    else
+        return (float)__builtin_bit_cast(_Float16, x);
+}
+
+// round to nearest even
+template <uint32_t TYPE>
+__device__ __forceinline__ typename Num<TYPE>::T num_round(float x) {
+    if constexpr (TYPE == TYPE_F32)
+        return __float_as_uint(x);
+    else if constexpr (TYPE == TYPE_BF16)
+        return __builtin_bit_cast(uint16_t, (__bf16)x);
+    else
+        return __builtin_bit_cast(uint16_t, (_Float16)x);
+}
+
+// One 16-byte vector of numbers in registers.
+template <uint32_t TYPE>
+struct Vec {
+    using N = Num<TYPE>;
+    using T = typename N::T;
+    uint32_t w[4];
+
+    __device__ __forceinline__ float get(uint32_t i) const {
+        const uint32_t x = w[i * 4 / N::VEC];
+        if constexpr (TYPE == TYPE_F32)
+            return __uint_as_float(x);
+        else if constexpr (TYPE == TYPE_BF16)
+            return __uint_as_float(i & 1 ? x & 0xffff0000u : x << 16);
+        else
+            return (float)__builtin_bit_cast(half2_t, x)[i & 1];
+    }
+    __device__ __forceinline__ void mask(uint32_t i) {  // element i := -inf
+        if constexpr (TYPE == TYPE_F32)
+            w[i] = N::NEG_INF;
+        else
+            w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | (N::NEG_INF << 16) : (w[i / 2] & 0xffff0000u) | N::NEG_INF;
+    }
+    // Makes the next use unpack anew, instead of numbers unpacked before in
+    // twice the registers.
+    __device__ __forceinline__ void keep_packed() {
+        if constexpr (TYPE != TYPE_F32) {
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) asm volatile("" : "+v"(w[i]));
+        }
+    }
+    __device__ __forceinline__ void fill_neg_inf() {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) w[i] = TYPE == TYPE_F32 ? N::NEG_INF : N::NEG_INF * 0x10001u;
+    }
+    __device__ __forceinline__ float max() const {
+        float m = get(0);
+#pragma unroll
+        for (uint32_t i = 1; i < N::VEC; ++i) m = fmaxf(m, get(i));
+        return m;
+    }
+    __device__ __forceinline__ void put(const float *x) {
+        if constexpr (TYPE == TYPE_F32) {
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) w[i] = __float_as_uint(x[i]);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                const float2_t f = {x[2 * i], x[2 * i + 1]};
+                if constexpr (TYPE == TYPE_BF16)
+                    w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf162_t));
+                else
+                    w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, half2_t));
+            }
+        }
+    }
+};
+
+// The vector at p[e .. e + VEC) with everything from element n on as -inf.
+// `avail` numbers can be read from p on, so that a vector which only its last
+// elements take out of the row is still one load; p is aligned to its type
+// alone (the hardware loads 16 bytes at any address).
+template <uint32_t TYPE>
+__device__ __forceinline__ Vec<TYPE> load_vec(const typename Num<TYPE>::T *p, uint32_t e, uint32_t n, uint64_t avail) {
+    constexpr uint32_t VEC = Num<TYPE>::VEC;
+    Vec<TYPE> v;
+    if (e >= n) {
+        v.fill_neg_inf();
+    } else if (e + VEC <= avail) {
+        __builtin_memcpy(v.w, p + e, 16);
+        if (e + VEC > n) {
+#pragma unroll
+            for (uint32_t i = 0; i < VEC; ++i)
+                if (e + i >= n) v.mask(i);
+        }
+    } else {
+        v.fill_neg_inf();
+        typename Num<TYPE>::T x[VEC];
+        __builtin_memcpy(x, v.w, 16);
+#pragma unroll
+        for (uint32_t i = 0; i < VEC; ++i)
+            if (e + i < n) x[i] = p[e + i];
+        __builtin_memcpy(v.w, x, 16);
+    }
+    return v;
+}
+
+// p[e .. min(e + VEC, n)) := x
+template <uint32_t TYPE>
+__device__ __forceinline__ void store_vec(typename Num<TYPE>::T *p, uint32_t e, uint32_t n, const float *x) {
+    constexpr uint32_t VEC = Num<TYPE>::VEC;
+    if (e + VEC <= n) {
+        Vec<TYPE> v;
+        v.put(x);
+        __builtin_memcpy(p + e, v.w, 16);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < VEC; ++i)
+            if (e + i < n) p[e + i] = num_round<TYPE>(x[i]);
+    }
+}
+
+// numbers from row r's start to the end of the matrix
+__device__ __forceinline__ uint64_t row_avail(const Matrix &m, uint64_t r) {
+    return (m.rows - 1 - r) * m.stride + m.cols;
+}
+
+// A number or an index whose type is known at run time only.
+__device__ __forceinline__ float load_num(const void *p, uint64_t i, uint32_t type) {
+    if (type == TYPE_F32) return ((const float *)p)[i];
+    const uint16_t x = ((const uint16_t *)p)[i];
+    return type == TYPE_BF16 ? num_float<TYPE_BF16>(x) : num_float<TYPE_F16>(x);
+}
+// an index below n, or n for any other
+__device__ __forceinline__ uint32_t load_index(const void *p, uint64_t i, uint32_t type, uint32_t n) {
+    if (type == INDEX_I32) {
+        const uint32_t x = ((const uint32_t *)p)[i];
+        return x < n ? x : n;
+    }
+    const uint64_t x = ((const uint64_t *)p)[i];
+    return x < n ? (uint32_t)x : n;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// ln of a sum: the exponent apart, so that the logarithm's own error stays
+// below 1e-7 however large the sum is
+__device__ __forceinline__ double ln_sum(double x) {
+    const int e = __builtin_amdgcn_frexp_exp(x);
+    const float f = (float)__builtin_amdgcn_frexp_mant(x);
+    return (double)e * 0.6931471805599453 + (double)logf(f);
+}
+
+__device__ __forceinline__ float wave_max_f(float v) {
+#pragma unroll
+    for (uint32_t o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
+__device__ __forceinline__ float wave_sum_f(float v) {
+#pragma unroll
+    for (uint32_t o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+// Block-wide maximum and sum; scratch holds NT / 64 words.  The sum's order is
+// fixed.  Every thread must call them; the scratch may be used again after the
+// caller's next barrier.
+template <uint32_t NT>
+__device__ __forceinline__ float block_max_f(float v, float *scratch) {
+    v = wave_max_f(v);
+    if ((threadIdx.x & 63u) == 0) scratch[threadIdx.x >> 6] = v;
+    lds_barrier();
+    v = scratch[0];
+#pragma unroll
+    for (uint32_t i = 1; i < NT / 64; ++i) v = fmaxf(v, scratch[i]);
+    return v;
+}
+template <uint32_t NT>
+__device__ __forceinline__ float block_sum_f(float v, float *scratch) {
+    v = wave_sum_f(v);
+    if ((threadIdx.x & 63u) == 0) scratch[threadIdx.x >> 6] = v;
+    lds_barrier();
+    v = scratch[0];
+#pragma unroll
+    for (uint32_t i = 1; i < NT / 64; ++i) v += scratch[i];
+    return v;
+}
+
+#endif  // __HIPCC__
+
+// How a row of `cols` numbers is cut: slices of `len` numbers for blocks of
+// NT threads that hold nv 16-byte vectors each.
+struct Slices {
+    uint32_t nv, len, n;
+};
+// The longest slices (fewest results to join) that give `blocks` blocks; 512
+// are two for each of the 256 CUs.
+inline Slices plan_slices(uint64_t rows, uint64_t cols, uint32_t vec, uint32_t threads, uint32_t nv_max,
+                          uint64_t blocks = 512) {
+    Slices s;
+    for (s.nv = nv_max;; s.nv /= 2) {
+        const uint64_t cap = (uint64_t)threads * s.nv * vec;
+        const uint64_t n = (cols + cap - 1) / cap;
+        if (rows * n < blocks && s.nv > 1) continue;
+        const uint64_t len = (cols + n - 1) / n;
+        s.len = (uint32_t)std::min<uint64_t>(cap, (len + vec - 1) / vec * vec);
+        s.n = (uint32_t)((cols + s.len - 1) / s.len);
+        return s;
+    }
+}
+
+// toplogits.hip
+constexpr uint32_t TOP_THREADS = 512, TOP_NV = 8;
+constexpr uint32_t TOP_JOIN = 2048;  // list entries that one block joins
+struct TopPlan {
+    Slices sl;
+    uint32_t fan;        // lists that one block joins
+    uint64_t lists[2];   // most lists that the two buffers hold per row
+    size_t bytes;
+};
+TopPlan plan_top(uint64_t rows, uint64_t cols, uint32_t k, uint32_t type);
+hipError_t launch_top(const Matrix &m, uint32_t k, float temperature, int32_t *idx_out, float *val_out,
+                      float *rest_out, const TopPlan &p, uint8_t *ws, hipStream_t s);
+
+// distill.hip
+struct Teacher {
+    const void *idx, *val;
+    const float *rest;
+    uint64_t idx_stride, val_stride;
+    uint32_t k, idx_type, val_type;
+};
+constexpr uint32_t DIST_THREADS = 256, DIST_NV = 8;
+size_t distill_ws_bytes(uint64_t rows, uint64_t cols, uint32_t type);
+hipError_t launch_distill_forward(const Matrix &m, const Teacher &t, float temperature, const float *weight,
+                                  float *loss_out, float *stats_out, uint8_t *ws, hipStream_t s);
+hipError_t launch_distill_backward(const Matrix &m, const Teacher &t, float temperature, const float *weight,
+                                   const float *upstream, uint64_t upstream_stride, const float *stats, void *grad,
+                                   uint64_t grad_stride, hipStream_t s);
+hipError_t launch_distill_step(const Matrix &m, const Teacher &t, float temperature, const float *weight,
+                               float *loss_out, void *grad, uint64_t grad_stride, uint8_t *ws, hipStream_t s);
+
+// balance.hip
+struct Routes {
+    const void *idx;
+    const uint8_t *mask;
+    uint64_t idx_stride;
+    uint32_t k, idx_type;
+    uint32_t group_rows, groups;
+};
+size_t balance_ws_bytes(uint64_t rows, uint64_t experts);
+hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, int32_t *counts_out,
+                                  int32_t *rows_out, float *prob_out, float *loss_out, uint8_t *ws, hipStream_t s);
+hipError_t launch_balance_backward(const Matrix &m, const Routes &r, float coef, const int32_t *counts,
+                                   const int32_t *count_rows, const int32_t *rows_in, const float *upstream,
+                                   void *grad, uint64_t grad_stride, hipStream_t s);
+
+}  // namespace dr

@@ -1,0 +1,407 @@
+// toplogits.hip -- the K largest logits of each row, and the logarithm of the
+// sum of exponentials over all others.
+//
+// A block holds one slice of a row in registers.  Its first look gives every
+// thread's largest logit; the ceil(K / 8)-th largest of them in each of the
+// eight waves bounds the slice's K-th largest logit from below, and the
+// smallest of the eight bounds serves all: at least K logits reach it, and
+// with numbers in no order only about 1.5 K do.  The second look lists those
+// in LDS and adds the exponentials of the others, so no sum is ever taken off
+// another one.  A listed logit's rank is the number of listed ones before it
+// (by value, then column), counted by one thread each; ranks from K on return
+// to the sum.  Where too many logits reach the bound (equal ones, say), the
+// exact K-th largest is found bit by bit instead.  Rows of several slices are
+// joined list by list in further launches.
+#include <type_traits>
+
+#include "launch.hpp"
+#include "losses.hpp"
+
+namespace dr {
+namespace {
+
+constexpr uint32_t NT = TOP_THREADS, NW = NT / 64;
+constexpr uint32_t CAND = 1024;  // listed logits per slice: four times the largest K
+
+// One row's payload, or one list of a join: `keys` hold the value's order key
+// above the complement of the column, so a larger key comes first and no two
+// are equal; 0 is no entry.
+struct TopArgs {
+    Matrix m;
+    Slices sl;
+    uint32_t k;
+    float c;      // log2(e) / temperature
+    float inv_t;  // 1 / temperature
+    uint64_t *keys;  // lists out: k keys each; null: the row's outputs
+    float2 *sums;    // and their (reference, sum of 2^((z - reference) c)) over what they leave out
+    int32_t *idx_out;
+    float *val_out, *rest_out;
+    // join only
+    const uint64_t *keys_in;
+    const float2 *sums_in;
+    uint32_t lists_in, fan;
+};
+
+__device__ __forceinline__ uint64_t top_key(float x, uint32_t col) {
+    // -0 counts as +0; NaN comes before all others
+    const uint32_t k = x != x ? 0xffffffffu : order_key(x + 0.f);
+    return (uint64_t)k << 32 | (0xffffffffu - col);
+}
+__device__ __forceinline__ float key_value(uint64_t key) { return order_key_inv((uint32_t)(key >> 32)); }
+
+// A float no larger than any whose order key has these upper 16 bits.
+__device__ __forceinline__ float key16_floor(uint32_t k16) {
+    return fmaxf(order_key_inv(k16 << 16), F_LOWEST);  // NaN patterns of -inf's neighbourhood become the lowest
+}
+
+// The n-th largest of the wave's 64 keys of 16 bits (1 <= n <= 64).
+__device__ __forceinline__ uint32_t wave_nth16(uint32_t key, uint32_t n) {
+    uint32_t t = 0;
+#pragma unroll
+    for (uint32_t b = 1u << 15; b != 0; b >>= 1)
+        if (popc64(ballot(key >= (t | b))) >= n) t |= b;
+    return t;
+}
+
+struct TopShared {
+    uint64_t cand[CAND], sorted[CAND];
+    uint32_t count;
+    uint32_t bound[NW];
+    uint32_t scan[NW + 1];
+    uint32_t bits[32];
+    float red[3][NW];
+};
+
+// (sum relative to reference a) as one relative to b >= a
+__device__ __forceinline__ float top_rescale(float x, float a, float b, float c) {
+    return x == 0.f ? 0.f : x * exp2_fast((a - b) * c);
+}
+
+// The end of a slice or a join: n sorted keys, and (ref, sum) of everything
+// else.  Writes the first K keys and returns the rest to the sum.
+__device__ __forceinline__ void top_finish(const TopArgs &a, uint64_t row, uint64_t list, const uint64_t *sorted,
+                                           uint32_t n, float ref, float sum, float *red) {
+    const uint32_t K = a.k;
+    if (n > K) {  // sorted[K] is the largest of what returns
+        const float first = key_value(sorted[K]), b = fmaxf(ref, first);
+        float back = 0.f;
+        for (uint32_t i = K + threadIdx.x; i < n; i += blockDim.x)
+            back += exp2_fast((key_value(sorted[i]) - b) * a.c);
+        back = wave_sum_f(back);
+        if ((threadIdx.x & 63u) == 0) red[threadIdx.x >> 6] = back;
+        lds_barrier();
+        sum = top_rescale(sum, ref, b, a.c);
+        for (uint32_t i = 0; i < blockDim.x / 64; ++i) sum += red[i];
+        ref = b;
+    }
+    if (a.keys) {
+        for (uint32_t i = threadIdx.x; i < K; i += blockDim.x) a.keys[list * K + i] = i < n ? sorted[i] : 0;
+        if (threadIdx.x == 0) a.sums[list] = make_float2(ref, sum);
+        return;
+    }
+    for (uint32_t i = threadIdx.x; i < K; i += blockDim.x) {
+        const uint64_t key = i < n ? sorted[i] : 0;
+        a.idx_out[row * K + i] = i < n ? (int32_t)(0xffffffffu - (uint32_t)key) : -1;
+        a.val_out[row * K + i] = i < n ? key_value(key) : F_NEG_INF;
+    }
+    if (threadIdx.x == 0 && a.rest_out)
+        a.rest_out[row] = sum > 0.f ? (float)((double)ref * (double)a.inv_t + ln_sum(sum)) : F_NEG_INF;
+}
+
+// A slice as the rare paths read it: again from memory, one vector per thread
+// and step, so that they cost the usual path no registers.
+template <uint32_t TYPE>
+struct SliceView {
+    const typename Num<TYPE>::T *p;
+    uint64_t avail;
+    uint32_t start, n;
+    static constexpr uint32_t STEP = NT * Num<TYPE>::VEC;
+
+    __device__ __forceinline__ Vec<TYPE> at(uint32_t e0) const {
+        return load_vec<TYPE>(p, e0 + threadIdx.x * Num<TYPE>::VEC, n, avail);
+    }
+    __device__ __forceinline__ uint32_t col(uint32_t e0, uint32_t e) const {
+        return start + e0 + threadIdx.x * Num<TYPE>::VEC + e;
+    }
+};
+
+// For a slice with more than CAND logits above -inf: lists exactly K, those
+// above the K-th largest, found bit by bit, and of those equal to it the ones
+// of lowest column.  Returns the K-th largest; *equal receives how many are
+// equal to it and not listed.
+template <uint32_t TYPE>
+__device__ __forceinline__ float top_exact(const SliceView<TYPE> &sl, uint32_t K, TopShared &sh, uint32_t *equal) {
+    constexpr uint32_t VEC = Num<TYPE>::VEC;
+    if (threadIdx.x < 32) sh.bits[threadIdx.x] = 0;
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    uint32_t t = 0;
+#pragma unroll 1
+    for (int b = 31; b >= 0; --b) {
+        const uint32_t want = t | 1u << b;
+        uint32_t n = 0;
+#pragma unroll 1
+        for (uint32_t e0 = 0; e0 < sl.n; e0 += sl.STEP) {
+            const Vec<TYPE> v = sl.at(e0);
+#pragma unroll
+            for (uint32_t e = 0; e < VEC; ++e) {
+                const uint32_t key = (uint32_t)(top_key(v.get(e), 0) >> 32);
+                n += key >= want && key > KEY_NEG_INF ? 1u : 0u;
+            }
+        }
+        n = wave_sum(n);
+        if ((threadIdx.x & 63u) == 0 && n) atomicAdd(&sh.bits[b], n);
+        __syncthreads();
+        if (sh.bits[b] >= K) t = want;
+    }
+#pragma unroll 1
+    for (uint32_t e0 = 0; e0 < sl.n; e0 += sl.STEP) {
+        const Vec<TYPE> v = sl.at(e0);
+#pragma unroll
+        for (uint32_t e = 0; e < VEC; ++e) {
+            const uint64_t key = top_key(v.get(e), sl.col(e0, e));
+            if ((uint32_t)(key >> 32) > t) sh.cand[atomicAdd(&sh.count, 1u)] = key;  // fewer than K
+        }
+    }
+    __syncthreads();
+    uint32_t have = sh.count, left = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (uint32_t e0 = 0; e0 < sl.n; e0 += sl.STEP) {  // columns ascend with the step, then the thread
+        const Vec<TYPE> v = sl.at(e0);
+        uint32_t n = 0, total;
+#pragma unroll
+        for (uint32_t e = 0; e < VEC; ++e) n += (uint32_t)(top_key(v.get(e), 0) >> 32) == t;
+        uint32_t at = have + block_excl_scan_n<NT>(n, sh.scan, &total);
+#pragma unroll
+        for (uint32_t e = 0; e < VEC; ++e) {
+            const uint64_t key = top_key(v.get(e), sl.col(e0, e));
+            if ((uint32_t)(key >> 32) == t) {
+                if (at < K) sh.cand[at] = key;
+                ++at;
+            }
+        }
+        const uint32_t take = min(total, K - have);
+        have += take;
+        left += total - take;
+    }
+    if (threadIdx.x == 0) sh.count = have;
+    __syncthreads();
+    *equal = left;
+    return order_key_inv(t);
+}
+
+// (reference, sum) of a slice's logits below the bound, relative to their own
+// largest; red: two sets of scratch.
+template <uint32_t TYPE>
+__device__ __forceinline__ float2 sum_below(const SliceView<TYPE> &sl, float bound, float c, float (*red)[NW]) {
+    constexpr uint32_t VEC = Num<TYPE>::VEC;
+    float mx = F_NEG_INF;
+#pragma unroll 1
+    for (uint32_t e0 = 0; e0 < sl.n; e0 += sl.STEP) {
+        const Vec<TYPE> v = sl.at(e0);
+#pragma unroll
+        for (uint32_t e = 0; e < VEC; ++e) mx = v.get(e) < bound ? fmaxf(mx, v.get(e)) : mx;
+    }
+    mx = block_max_f<NT>(mx, red[0]);
+    const float ref = mx == F_NEG_INF ? 0.f : mx;
+    float sum = 0.f;
+#pragma unroll 1
+    for (uint32_t e0 = 0; e0 < sl.n; e0 += sl.STEP) {
+        const Vec<TYPE> v = sl.at(e0);
+#pragma unroll
+        for (uint32_t e = 0; e < VEC; ++e) sum += v.get(e) < bound ? exp2_fast((v.get(e) - ref) * c) : 0.f;
+    }
+    return make_float2(mx, block_sum_f<NT>(sum, red[1]));
+}
+
+template <uint32_t TYPE, int NV>
+__global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
+    using N = Num<TYPE>;
+    constexpr uint32_t VEC = N::VEC;
+    __shared__ TopShared sh;
+    const uint64_t row = blockIdx.x / a.sl.n;
+    const uint32_t s = blockIdx.x % a.sl.n, start = s * a.sl.len, n = min(a.sl.len, a.m.cols - start);
+    const auto *p = (const typename N::T *)a.m.p + row * a.m.stride + start;
+    const uint64_t avail = row_avail(a.m, row) - start;
+    const SliceView<TYPE> sl = {p, avail, start, n};
+    Vec<TYPE> v[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = load_vec<TYPE>(p, (i * NT + threadIdx.x) * VEC, n, avail);
+    if (threadIdx.x == 0) sh.count = 0;
+    float mx = F_NEG_INF;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) mx = fmaxf(mx, v[i].max());
+    const uint32_t nth = wave_nth16(order_key(mx) >> 16, (a.k + NW - 1) / NW);
+    if ((threadIdx.x & 63u) == 0) sh.bound[threadIdx.x >> 6] = nth;
+    lds_barrier();
+    uint32_t low = sh.bound[0];
+#pragma unroll
+    for (uint32_t i = 1; i < NW; ++i) low = min(low, sh.bound[i]);
+    float bound = key16_floor(low);
+    // list what reaches the bound, add the others' exponentials relative to it
+    float ref = bound, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        v[i].keep_packed();
+#pragma unroll
+        for (uint32_t e = 0; e < VEC; ++e) {
+            float x = v[i].get(e);
+            if (!(x < bound)) {
+                const uint32_t at = atomicAdd(&sh.count, 1u);
+                if (at < CAND) sh.cand[at] = top_key(x, start + (i * NT + threadIdx.x) * VEC + e);
+                x = F_NEG_INF;
+            }
+            sum += exp2_fast((x - ref) * a.c);
+        }
+    }
+    __syncthreads();
+    uint32_t count = sh.count, equal = 0;
+    sum = block_sum_f<NT>(sum, sh.red[0]);
+    const bool exact = count > CAND;
+    if (exact) {
+        bound = top_exact<TYPE>(sl, a.k, sh, &equal);
+        count = sh.count;
+    }
+    // other logits than these are listed, or all that was added lies far below the bound
+    if (exact || !(sum > 1e-30f)) {
+        const float2 x = sum_below<TYPE>(sl, bound, a.c, sh.red + 1);
+        ref = x.x;
+        sum = x.y;
+        if (equal) {
+            sum = top_rescale(sum, ref, bound, a.c) + (float)equal;
+            ref = bound;
+        }
+        __syncthreads();
+    }
+    // ranks
+    for (uint32_t i = threadIdx.x; i < count; i += NT) {
+        const uint64_t key = sh.cand[i];
+        uint32_t rank = 0;
+        for (uint32_t j = 0; j < count; ++j) rank += sh.cand[j] > key ? 1u : 0u;
+        sh.sorted[rank] = key;
+    }
+    __syncthreads();
+    top_finish(a, row, (uint64_t)blockIdx.x, sh.sorted, count, ref, sum, sh.red[1]);
+}
+
+// `fan` sorted lists of a row into one.  An entry's rank is its place in its
+// own list and, by binary search, the entries of every other list before it.
+constexpr uint32_t JT = 256;
+__global__ __launch_bounds__(JT) void k_top_join(TopArgs a) {
+    __shared__ uint64_t in[TOP_JOIN], sorted[TOP_JOIN];
+    __shared__ float red[JT / 64];
+    const uint32_t groups = (a.lists_in + a.fan - 1) / a.fan, K = a.k;
+    const uint64_t row = blockIdx.x / groups;
+    const uint32_t first = blockIdx.x % groups * a.fan, lists = min(a.fan, a.lists_in - first);
+    const uint64_t from = row * a.lists_in + first;
+    for (uint32_t i = threadIdx.x; i < lists * K; i += JT) in[i] = a.keys_in[from * K + i];
+    float ref = F_NEG_INF, sum = 0.f;
+    for (uint32_t i = 0; i < lists; ++i)
+        if (a.sums_in[from + i].y > 0.f) ref = fmaxf(ref, a.sums_in[from + i].x);
+    for (uint32_t i = 0; i < lists; ++i) {
+        const float2 x = a.sums_in[from + i];
+        sum += top_rescale(x.y, x.x, ref, a.c);
+    }
+    __syncthreads();
+    uint32_t total = 0;
+    for (uint32_t i = threadIdx.x; i < lists * K; i += JT) {
+        const uint64_t key = in[i];
+        if (!key) continue;
+        const uint32_t own = i / K;
+        uint32_t rank = i - own * K;
+        for (uint32_t l = 0; l < lists; ++l) {
+            if (l == own) continue;
+            uint32_t lo = 0, hi = K;  // entries of list l above the key
+            while (lo < hi) {
+                const uint32_t mid = (lo + hi) / 2;
+                if (in[l * K + mid] > key)
+                    lo = mid + 1;
+                else
+                    hi = mid;
+            }
+            rank += lo;
+        }
+        sorted[rank] = key;
+        ++total;
+    }
+    __shared__ uint32_t entries;
+    if (threadIdx.x == 0) entries = 0;
+    __syncthreads();
+    total = wave_sum(total);
+    if ((threadIdx.x & 63u) == 0 && total) atomicAdd(&entries, total);
+    __syncthreads();
+    top_finish(a, row, (uint64_t)blockIdx.x, sorted, entries, ref, sum, red);
+}
+
+template <uint32_t TYPE>
+void slice_kernel(const TopArgs &a, hipStream_t s) {
+    const uint32_t grid = (uint32_t)(a.m.rows * a.sl.n);
+    switch (a.sl.nv) {
+        case 1: k_top_slice<TYPE, 1><<<grid, NT, 0, s>>>(a); break;
+        case 2: k_top_slice<TYPE, 2><<<grid, NT, 0, s>>>(a); break;
+        case 4: k_top_slice<TYPE, 4><<<grid, NT, 0, s>>>(a); break;
+        default: k_top_slice<TYPE, 8><<<grid, NT, 0, s>>>(a); break;
+    }
+    trace_mark(s, "k_top_slice");
+}
+
+uint64_t list_bytes(uint64_t rows, uint64_t lists, uint32_t k) {
+    return (rows * lists * (k * sizeof(uint64_t) + sizeof(float2)) + 255) / 256 * 256;
+}
+
+}  // namespace
+
+TopPlan plan_top(uint64_t rows, uint64_t cols, uint32_t k, uint32_t type) {
+    TopPlan p = {};
+    p.sl = plan_slices(rows, cols, 16 / type_bytes(type), TOP_THREADS, TOP_NV);
+    p.fan = std::max(2u, TOP_JOIN / k);
+    p.lists[0] = p.sl.n > 1 ? p.sl.n : 0;
+    p.lists[1] = p.sl.n > p.fan ? (p.sl.n + p.fan - 1) / p.fan : 0;
+    p.bytes = list_bytes(rows, p.lists[0], k) + list_bytes(rows, p.lists[1], k);
+    return p;
+}
+
+hipError_t launch_top(const Matrix &m, uint32_t k, float temperature, int32_t *idx_out, float *val_out,
+                      float *rest_out, const TopPlan &p, uint8_t *ws, hipStream_t s) {
+    TopArgs a = {};
+    a.m = m;
+    a.sl = p.sl;
+    a.k = k;
+    a.c = (float)(1.4426950408889634074 / temperature);
+    a.inv_t = (float)(1.0 / temperature);
+    a.idx_out = idx_out;
+    a.val_out = val_out;
+    a.rest_out = rest_out;
+    uint64_t *keys[2];
+    float2 *sums[2];
+    for (int i = 0; i < 2; ++i) {
+        keys[i] = (uint64_t *)(ws + (i ? list_bytes(m.rows, p.lists[0], k) : 0));
+        sums[i] = (float2 *)(keys[i] + m.rows * p.lists[i] * k);
+    }
+    if (p.sl.n > 1) {
+        a.keys = keys[0];
+        a.sums = sums[0];
+    }
+    switch (m.type) {
+        case TYPE_F32: slice_kernel<TYPE_F32>(a, s); break;
+        case TYPE_BF16: slice_kernel<TYPE_BF16>(a, s); break;
+        default: slice_kernel<TYPE_F16>(a, s); break;
+    }
+    uint32_t lists = p.sl.n;
+    for (int from = 0; lists > 1; from ^= 1) {
+        const uint32_t groups = (lists + p.fan - 1) / p.fan;
+        a.keys_in = keys[from];
+        a.sums_in = sums[from];
+        a.lists_in = lists;
+        a.fan = p.fan;
+        a.keys = groups > 1 ? keys[from ^ 1] : nullptr;
+        a.sums = groups > 1 ? sums[from ^ 1] : nullptr;
+        k_top_join<<<(uint32_t)(m.rows * groups), JT, 0, s>>>(a);
+        trace_mark(s, "k_top_join");
+        lists = groups;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace dr
