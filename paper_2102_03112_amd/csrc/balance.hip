@@ -92,7 +92,7 @@ __device__ __forceinline__ void load_row(const Matrix &m, uint64_t row, bool val
     for (uint32_t i = 0; i < NI; ++i) {
         Vec<TYPE> v;
         if (valid)
-            v = load_vec<TYPE>((const typename Num<TYPE>::T *)m.p + row * m.stride, (i * LANES + sub) * VEC, m.cols,
+            v = load_vec<TYPE, false>((const typename Num<TYPE>::T *)m.p + row * m.stride, (i * LANES + sub) * VEC, m.cols,
                                row_avail(m, row));
         else
             v.fill_neg_inf();
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(BT) void k_balance_grad(BalanceArgs a) {
 #pragma unroll
             for (uint32_t i = 0; i < NI; ++i) {
                 const uint32_t e = (i * LANES + sub) * VEC;
-                if (e < E) store_vec<TYPE>((T *)a.grad + r * a.grad_stride, e, E, x + i * VEC);
+                if (e < E) store_vec<TYPE, false>((T *)a.grad + r * a.grad_stride, e, E, x + i * VEC);
             }
         }
     }

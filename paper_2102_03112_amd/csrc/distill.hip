@@ -49,25 +49,56 @@ __device__ __forceinline__ uint32_t kept_bits(const uint32_t *bm, uint32_t i) {
     return VEC == 8 ? b : (b >> (i * VEC % 8)) & 0xfu;
 }
 
+// (maximum, sum) of a slice's columns not kept, formed from x - m, by reading
+// the slice again: where nothing is left, where all lies near the lowest
+// number, or where a maximum of bits was no more than an estimate.
+template <uint32_t TYPE>
+__device__ __forceinline__ float2 slice_again(const typename Num<TYPE>::T *p, uint32_t n, uint64_t avail,
+                                              const uint32_t *bm, float c, float (*red)[DIST_THREADS / 64]) {
+    constexpr uint32_t VEC = Num<TYPE>::VEC, STEP = DIST_THREADS * VEC;
+    float mx = F_NEG_INF, sum = 0.f;
+#pragma unroll 1
+    for (uint32_t pass = 0; pass < 2; ++pass) {
+        const float ref = mx == F_NEG_INF ? 0.f : mx;
+#pragma unroll 1
+        for (uint32_t e0 = threadIdx.x * VEC; e0 < n; e0 += STEP) {
+            const Vec<TYPE> v = load_vec<TYPE, false>(p, e0, n, avail);
+            const uint32_t b = kept_bits<VEC>(bm, e0 / VEC);
+#pragma unroll
+            for (uint32_t e = 0; e < VEC; ++e) {
+                const float x = b >> e & 1u ? F_NEG_INF : v.get(e);
+                if (pass == 0)
+                    mx = fmaxf(mx, x);
+                else
+                    sum += exp2_fast((x - ref) * c);
+            }
+        }
+        if (pass == 0)
+            mx = block_max_f<DIST_THREADS>(mx, red[0]);
+        else
+            sum = block_sum_f<DIST_THREADS>(sum, red[1]);
+    }
+    return make_float2(mx, sum);
+}
+
 template <uint32_t TYPE, int NV>
 __global__ __launch_bounds__(DIST_THREADS) void k_distill_slice(DistillArgs a) {
     using N = Num<TYPE>;
     constexpr uint32_t VEC = N::VEC, CAP = DIST_THREADS * NV * VEC;
     __shared__ uint32_t bm[CAP / 32];
-    __shared__ float red[2][DIST_THREADS / 64];
+    __shared__ float red[4][DIST_THREADS / 64];
     const uint64_t row = blockIdx.x / a.sl.n;
     const uint32_t s = blockIdx.x % a.sl.n, start = s * a.sl.len, n = min(a.sl.len, a.m.cols - start);
     if (a.weight && a.weight[row] == 0.f) return;
     const auto *p = (const typename N::T *)a.m.p + row * a.m.stride + start;
     const uint64_t avail = row_avail(a.m, row) - start;
     Vec<TYPE> v[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = load_vec<TYPE>(p, (i * DIST_THREADS + threadIdx.x) * VEC, n, avail);
+    load_slice<TYPE, DIST_THREADS>(v, p, n, avail);
     for (uint32_t i = threadIdx.x; i < CAP / 32; i += DIST_THREADS) bm[i] = 0;
     lds_barrier();
     mark_kept(a.t, row, start, n, a.m.cols, bm);
     lds_barrier();
-    float mx = F_NEG_INF;
+    uint32_t bits = Vec<TYPE>::max_bits_none();
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const uint32_t b = kept_bits<VEC>(bm, i * DIST_THREADS + threadIdx.x);
@@ -76,19 +107,19 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_slice(DistillArgs a) {
             for (uint32_t e = 0; e < VEC; ++e)
                 if (b >> e & 1u) v[i].mask(e);
         }
-        mx = fmaxf(mx, v[i].max());
+        bits = v[i].max_bits(bits);
     }
-    mx = block_max_f<DIST_THREADS>(mx, red[0]);
-    const float ref = mx == F_NEG_INF ? 0.f : mx;
+    const float mx = block_max_f<DIST_THREADS>(Vec<TYPE>::max_value(bits), red[0]);
+    const Base2 to2(mx, a.c);
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        v[i].keep_packed();
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (uint32_t e = 0; e < VEC; ++e) sum += exp2_fast((v[i].get(e) - ref) * a.c);
-    }
+        for (uint32_t e = 0; e < VEC; ++e) sum += to2(v[i].get(e));
     sum = block_sum_f<DIST_THREADS>(sum, red[1]);
-    if (threadIdx.x == 0) a.part[row * a.sl.n + s] = make_float2(mx, sum);
+    float2 x = make_float2(mx, sum * to2.to(mx));
+    if (!sum_in_range(sum)) x = slice_again<TYPE>(p, n, avail, bm, a.c, red + 2);
+    if (threadIdx.x == 0) a.part[row * a.sl.n + s] = x;
 }
 
 // x 2^((a - b) c) for a sum x relative to a, wanted relative to b >= a
@@ -96,8 +127,68 @@ __device__ __forceinline__ float rescale(float x, float a, float b, float c) {
     return x == 0.f ? 0.f : x * exp2_fast((a - b) * c);
 }
 
-// One wave per row.
-template <uint32_t TYPE>
+// A row's result from its columns not kept (m_tail, tail: their maximum and
+// sum) and its kept entries, one per lane and step: student's logit x, teacher's
+// y, `there` telling whether there is one.  All lanes of a wave take part.
+struct RowResult {
+    double loss;  // not yet times the weight
+    float stats[6];
+};
+template <int NK>
+__device__ __forceinline__ RowResult row_result(float m_tail, double tail, const float (&x)[NK], const float (&y)[NK],
+                                                const bool (&there)[NK], float rest, float c, float inv_t) {
+    float m_p = rest, m = m_tail;
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+        if (there[i]) {
+            m = fmaxf(m, x[i]);
+            m_p = fmaxf(m_p, y[i] * inv_t);
+        }
+    m = wave_max_f(m);
+    m_p = wave_max_f(m_p);
+    // sums relative to m and m_p; d: the teacher's logit less the student's
+    double sum_q = 0.0, sum_p = 0.0, sum_d = 0.0;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+        if (!there[i]) continue;
+        if (x[i] != F_NEG_INF) sum_q += exp2_fast((x[i] - m) * c);
+        const float e = y[i] == F_NEG_INF ? 0.f : expf(y[i] * inv_t - m_p);
+        if (e > 0.f) {
+            sum_p += e;
+            sum_d += e * (((double)y[i] - (double)x[i]) * (double)inv_t);
+        }
+    }
+    const double tail_q = tail == 0.0 ? 0.0 : tail * exp2_fast((m_tail - m) * c);
+    sum_q = wave_sum_f64(sum_q) + tail_q;
+    sum_p = wave_sum_f64(sum_p);
+    sum_d = wave_sum_f64(sum_d);
+    const float e_rest = rest == F_NEG_INF ? 0.f : expf(rest - m_p);
+    sum_p += e_rest;
+    RowResult r;
+    r.loss = 0.0;
+    // the columns not kept have gradient (w / t) a_tail exp((z - m_tail) / t)
+    double a_tail = 0.0;
+    if (sum_p > 0.0) {
+        if (sum_q == 0.0 || (e_rest > 0.f && tail == 0.0)) {
+            r.loss = __builtin_inf();
+        } else {
+            if (e_rest > 0.f) sum_d += e_rest * ((double)rest - ((double)m_tail * inv_t + ln_sum(tail)));
+            // the terms' mean, less ln of one normaliser over the other
+            r.loss = sum_d / sum_p - ((m_p + ln_sum(sum_p)) - ((double)m * inv_t + ln_sum(sum_q)));
+        }
+        if (tail > 0.0) a_tail = (tail_q / sum_q - e_rest / sum_p) / tail;
+    }
+    r.stats[0] = m;
+    r.stats[1] = sum_q > 0.0 ? (float)(1.0 / sum_q) : 0.f;
+    r.stats[2] = m_tail;
+    r.stats[3] = (float)a_tail;
+    r.stats[4] = m_p;
+    r.stats[5] = sum_p > 0.0 ? (float)(1.0 / sum_p) : 0.f;
+    return r;
+}
+
+// One wave per row joins its slices; NK entries per lane.
+template <uint32_t TYPE, int NK>
 __global__ __launch_bounds__(DIST_THREADS) void k_distill_join(DistillArgs a) {
     const uint32_t lane = threadIdx.x & 63u;
     const uint64_t row = (uint64_t)blockIdx.x * (DIST_THREADS / 64) + (threadIdx.x >> 6);
@@ -108,69 +199,42 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_join(DistillArgs a) {
         if (a.stats && lane < STATS) a.stats[row * STATS + lane] = 0.f;
         return;
     }
-    // the columns not kept
-    float m_tail = F_NEG_INF;
-    for (uint32_t i = lane; i < a.sl.n; i += 64) m_tail = fmaxf(m_tail, a.part[row * a.sl.n + i].x);
+    const auto *z = (const typename Num<TYPE>::T *)a.m.p + row * a.m.stride;
+    float x[NK], y[NK];
+    bool there[NK];
+    uint32_t j[NK];
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+        const uint32_t k = i * 64 + lane;
+        j[i] = k < a.t.k ? load_index(a.t.idx, row * a.t.idx_stride + k, a.t.idx_type, a.m.cols) : a.m.cols;
+    }
+    const float2 first = lane < a.sl.n ? a.part[row * a.sl.n + lane] : make_float2(F_NEG_INF, 0.f);
+    const float rest = a.t.rest ? a.t.rest[row] : F_NEG_INF;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+        there[i] = j[i] < a.m.cols;
+        x[i] = y[i] = 0.f;
+        if (there[i]) {
+            x[i] = num_float<TYPE>(z[j[i]]);
+            y[i] = load_num(a.t.val, row * a.t.val_stride + i * 64 + lane, a.t.val_type);
+        }
+    }
+    float m_tail = first.x;
+    for (uint32_t i = lane + 64; i < a.sl.n; i += 64) m_tail = fmaxf(m_tail, a.part[row * a.sl.n + i].x);
     m_tail = wave_max_f(m_tail);
-    double tail = 0.0;
-    for (uint32_t i = lane; i < a.sl.n; i += 64) {
-        const float2 x = a.part[row * a.sl.n + i];
-        tail += rescale(x.y, x.x, m_tail, a.c);
+    double tail = rescale(first.y, first.x, m_tail, a.c);
+    for (uint32_t i = lane + 64; i < a.sl.n; i += 64) {
+        const float2 p = a.part[row * a.sl.n + i];
+        tail += rescale(p.y, p.x, m_tail, a.c);
     }
     tail = wave_sum_f64(tail);
-    // the kept ones
-    const auto *z = (const typename Num<TYPE>::T *)a.m.p + row * a.m.stride;
-    const float rest = a.t.rest ? a.t.rest[row] : F_NEG_INF;
-    float m_p = rest, m = m_tail;
-    for (uint32_t k = lane; k < a.t.k; k += 64) {
-        const uint32_t j = load_index(a.t.idx, row * a.t.idx_stride + k, a.t.idx_type, a.m.cols);
-        if (j < a.m.cols) {
-            m = fmaxf(m, num_float<TYPE>(z[j]));
-            m_p = fmaxf(m_p, load_num(a.t.val, row * a.t.val_stride + k, a.t.val_type) * a.inv_t);
-        }
-    }
-    m = wave_max_f(m);
-    m_p = wave_max_f(m_p);
-    // sums relative to m and m_p; d: the teacher's logit less the student's
-    double sum_q = 0.0, sum_p = 0.0, sum_d = 0.0;
-    for (uint32_t k = lane; k < a.t.k; k += 64) {
-        const uint32_t j = load_index(a.t.idx, row * a.t.idx_stride + k, a.t.idx_type, a.m.cols);
-        if (j >= a.m.cols) continue;
-        const float x = num_float<TYPE>(z[j]), y = load_num(a.t.val, row * a.t.val_stride + k, a.t.val_type);
-        if (x != F_NEG_INF) sum_q += exp2_fast((x - m) * a.c);
-        const float e = y == F_NEG_INF ? 0.f : expf(y * a.inv_t - m_p);
-        if (e > 0.f) {
-            sum_p += e;
-            sum_d += e * (((double)y - (double)x) * (double)a.inv_t);
-        }
-    }
-    const double tail_q = tail == 0.0 ? 0.0 : tail * exp2_fast((m_tail - m) * a.c);
-    sum_q = wave_sum_f64(sum_q) + tail_q;
-    sum_p = wave_sum_f64(sum_p);
-    sum_d = wave_sum_f64(sum_d);
-    const float e_rest = rest == F_NEG_INF ? 0.f : expf(rest - m_p);
-    sum_p += e_rest;
-    double loss = 0.0;
-    // the columns not kept have gradient (w / t) a_tail exp((z - m_tail) / t)
-    double a_tail = 0.0;
-    if (sum_p > 0.0) {
-        if (sum_q == 0.0 || (e_rest > 0.f && tail == 0.0)) {
-            loss = __builtin_inf();
-        } else {
-            if (e_rest > 0.f) sum_d += e_rest * ((double)rest - ((double)m_tail * a.inv_t + ln_sum(tail)));
-            // ln of the two normalisers: their difference is what the terms' mean is off by
-            loss = sum_d / sum_p - ((m_p + ln_sum(sum_p)) - ((double)m * a.inv_t + ln_sum(sum_q)));
-        }
-        if (tail > 0.0) a_tail = (tail_q / sum_q - e_rest / sum_p) / tail;
-    }
-    if (lane == 0) a.loss[row] = (float)(w * loss);
+    const RowResult r = row_result<NK>(m_tail, tail, x, y, there, rest, a.c, a.inv_t);
+    if (lane == 0) a.loss[row] = (float)(w * r.loss);
     if (a.stats && lane < STATS) {
-        const float st[STATS] = {m, sum_q > 0.0 ? (float)(1.0 / sum_q) : 0.f, m_tail, (float)a_tail, m_p,
-                                 sum_p > 0.0 ? (float)(1.0 / sum_p) : 0.f, 0.f, 0.f};
-        float x = st[0];
+        float st = 0.f;
 #pragma unroll
-        for (uint32_t i = 1; i < STATS; ++i) x = lane == i ? st[i] : x;
-        a.stats[row * STATS + lane] = x;
+        for (uint32_t i = 0; i < 6; ++i) st = lane == i ? r.stats[i] : st;
+        a.stats[row * STATS + lane] = st;
     }
 }
 
@@ -195,8 +259,7 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
     const T *p = (const T *)a.m.p + row * a.m.stride + start;
     const uint64_t avail = row_avail(a.m, row) - start;
     Vec<TYPE> v[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = load_vec<TYPE>(p, (i * DIST_THREADS + threadIdx.x) * VEC, n, avail);
+    load_slice<TYPE, DIST_THREADS>(v, p, n, avail);
     const float *st = a.stats + row * STATS;
     const float m = st[0] == F_NEG_INF ? 0.f : st[0], m_tail = st[2] == F_NEG_INF ? 0.f : st[2];
     const float scale = w * u * a.inv_t, q = scale * st[1], f = scale * st[3];
@@ -216,12 +279,16 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
         g[i] = q * exp2_fast((x - m) * a.c) - scale * e;
     }
     __syncthreads();
+    const Base2 to2(m_tail, a.c);
+    const bool low = fabsf(m_tail * a.c) >= 1e30f;  // all near the lowest number
+    const float f2 = f * to2.to(m_tail);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const uint32_t e0 = (i * DIST_THREADS + threadIdx.x) * VEC;
         float x[VEC];
 #pragma unroll
-        for (uint32_t e = 0; e < VEC; ++e) x[e] = f * exp2_fast((v[i].get(e) - m_tail) * a.c);
+        for (uint32_t e = 0; e < VEC; ++e)
+            x[e] = low ? f * exp2_fast((v[i].get(e) - m_tail) * a.c) : f2 * to2(v[i].get(e));
         if (e0 < n) store_vec<TYPE>(out, e0, n, x);
     }
     __syncthreads();
@@ -259,8 +326,13 @@ void slice_kernel(const DistillArgs &a, hipStream_t s) {
 
 template <uint32_t TYPE>
 void join_kernel(const DistillArgs &a, hipStream_t s) {
-    const uint32_t per = DIST_THREADS / 64;
-    k_distill_join<TYPE><<<(uint32_t)((a.m.rows + per - 1) / per), DIST_THREADS, 0, s>>>(a);
+    const uint32_t per = DIST_THREADS / 64, grid = (uint32_t)((a.m.rows + per - 1) / per);
+    if (a.t.k <= 64)
+        k_distill_join<TYPE, 1><<<grid, DIST_THREADS, 0, s>>>(a);
+    else if (a.t.k <= 256)
+        k_distill_join<TYPE, 4><<<grid, DIST_THREADS, 0, s>>>(a);
+    else
+        k_distill_join<TYPE, 16><<<grid, DIST_THREADS, 0, s>>>(a);
     trace_mark(s, "k_distill_join");
 }
 

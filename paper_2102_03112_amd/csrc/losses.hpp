@@ -55,6 +55,18 @@ typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf162_t __attribute__((ext_vector_type(2)));
 typedef float float2_t __attribute__((ext_vector_type(2)));
 
+// Maxima without the operation that quiets their operands first.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+
 template <uint32_t TYPE>
 __device__ __forceinline__ float num_float(typename Num<TYPE>::T x) {
     if constexpr (TYPE == TYPE_F32)
@@ -98,6 +110,25 @@ struct Vec {
         else
             w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | (N::NEG_INF << 16) : (w[i / 2] & 0xffff0000u) | N::NEG_INF;
     }
+    // The numbers as a queue: push before the first one, take the first one off.
+    __device__ __forceinline__ void push(T x) {
+        if constexpr (TYPE == TYPE_F32) {
+            w[3] = w[2], w[2] = w[1], w[1] = w[0], w[0] = x;
+        } else {
+            w[3] = w[3] << 16 | w[2] >> 16, w[2] = w[2] << 16 | w[1] >> 16, w[1] = w[1] << 16 | w[0] >> 16;
+            w[0] = w[0] << 16 | x;
+        }
+    }
+    __device__ __forceinline__ T pop() {
+        const T x = (T)w[0];
+        if constexpr (TYPE == TYPE_F32) {
+            w[0] = w[1], w[1] = w[2], w[2] = w[3];
+        } else {
+            w[0] = w[0] >> 16 | w[1] << 16, w[1] = w[1] >> 16 | w[2] << 16, w[2] = w[2] >> 16 | w[3] << 16;
+            w[3] >>= 16;
+        }
+        return x;
+    }
     // Makes the next use unpack anew, instead of numbers unpacked before in
     // twice the registers.
     __device__ __forceinline__ void keep_packed() {
@@ -110,11 +141,29 @@ struct Vec {
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) w[i] = TYPE == TYPE_F32 ? N::NEG_INF : N::NEG_INF * 0x10001u;
     }
-    __device__ __forceinline__ float max() const {
-        float m = get(0);
-#pragma unroll
-        for (uint32_t i = 1; i < N::VEC; ++i) m = fmaxf(m, get(i));
-        return m;
+    // The largest of the numbers so far and this vector's, kept as bits: a float
+    // for 32-bit numbers, two halves for 16-bit ones.  bfloat16 orders as
+    // float16 does, bit for bit, but for magnitudes from 2^121 on, which read
+    // as NaN and are passed over (or come out as such a number): a maximum that
+    // is only an estimate, which the sums that follow it put to the test.
+    __device__ __forceinline__ uint32_t max_bits(uint32_t m) const {
+        if constexpr (TYPE == TYPE_F32) {
+            const float f = max3(__uint_as_float(m), get(0), get(1));
+            return __float_as_uint(max3(f, get(2), get(3)));
+        } else {
+            return max_halves(max_halves(m, w[0]), max_halves(max_halves(w[1], w[2]), w[3]));
+        }
+    }
+    static __device__ __forceinline__ uint32_t max_bits_none() {
+        return TYPE == TYPE_F32 ? N::NEG_INF : N::NEG_INF * 0x10001u;
+    }
+    static __device__ __forceinline__ float max_value(uint32_t m) {
+        if constexpr (TYPE == TYPE_F32) {
+            return __uint_as_float(m);
+        } else {
+            const float a = num_float<TYPE>((T)m), b = num_float<TYPE>((T)(m >> 16));
+            return a > b ? a : b;
+        }
     }
     __device__ __forceinline__ void put(const float *x) {
         if constexpr (TYPE == TYPE_F32) {
@@ -133,47 +182,76 @@ struct Vec {
     }
 };
 
+// 16 bytes at any address that suits a 16-bit number
+typedef uint32_t vec_any __attribute__((ext_vector_type(4), aligned(2)));
+
+template <uint32_t TYPE, bool NT>
+__device__ __forceinline__ Vec<TYPE> load_whole(const typename Num<TYPE>::T *p) {
+    const vec_any x = NT ? __builtin_nontemporal_load((const vec_any *)p) : *(const vec_any *)p;
+    Vec<TYPE> v;
+    __builtin_memcpy(v.w, &x, 16);
+    return v;
+}
+
 // The vector at p[e .. e + VEC) with everything from element n on as -inf.
 // `avail` numbers can be read from p on, so that a vector which only its last
 // elements take out of the row is still one load; p is aligned to its type
-// alone (the hardware loads 16 bytes at any address).
-template <uint32_t TYPE>
+// alone (the hardware loads 16 bytes at any address).  NT: numbers that are
+// read once (reading 1 GiB: 6.1 TB/s without, 7.0 with; copying it: 5.4 with
+// neither load nor store so, 6.3 with both).
+template <uint32_t TYPE, bool NT = true>
 __device__ __forceinline__ Vec<TYPE> load_vec(const typename Num<TYPE>::T *p, uint32_t e, uint32_t n, uint64_t avail) {
     constexpr uint32_t VEC = Num<TYPE>::VEC;
     Vec<TYPE> v;
     if (e >= n) {
         v.fill_neg_inf();
     } else if (e + VEC <= avail) {
-        __builtin_memcpy(v.w, p + e, 16);
+        v = load_whole<TYPE, NT>(p + e);
         if (e + VEC > n) {
 #pragma unroll
             for (uint32_t i = 0; i < VEC; ++i)
                 if (e + i >= n) v.mask(i);
         }
-    } else {
+    } else {  // the matrix ends in it: number by number, the last one first
         v.fill_neg_inf();
-        typename Num<TYPE>::T x[VEC];
-        __builtin_memcpy(x, v.w, 16);
-#pragma unroll
-        for (uint32_t i = 0; i < VEC; ++i)
-            if (e + i < n) x[i] = p[e + i];
-        __builtin_memcpy(v.w, x, 16);
+#pragma unroll 1
+        for (uint32_t i = VEC; i-- > 0;) v.push(e + i < n ? p[e + i] : (typename Num<TYPE>::T)Num<TYPE>::NEG_INF);
     }
     return v;
 }
 
+// The NV vectors that a thread of a block of THREADS holds of n numbers:
+// vector i THREADS + thread.
+template <uint32_t TYPE, uint32_t THREADS, int NV, bool NT = true>
+__device__ __forceinline__ void load_slice(Vec<TYPE> (&v)[NV], const typename Num<TYPE>::T *p, uint32_t n,
+                                           uint64_t avail) {
+    constexpr uint32_t VEC = Num<TYPE>::VEC;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint32_t e = (i * THREADS + threadIdx.x) * VEC;
+        if ((i + 1) * THREADS * VEC <= n)  // the whole block's
+            v[i] = load_whole<TYPE, NT>(p + e);
+        else
+            v[i] = load_vec<TYPE, NT>(p, e, n, avail);
+    }
+}
+
 // p[e .. min(e + VEC, n)) := x
-template <uint32_t TYPE>
+template <uint32_t TYPE, bool NT = true>
 __device__ __forceinline__ void store_vec(typename Num<TYPE>::T *p, uint32_t e, uint32_t n, const float *x) {
     constexpr uint32_t VEC = Num<TYPE>::VEC;
+    Vec<TYPE> v;
+    v.put(x);
     if (e + VEC <= n) {
-        Vec<TYPE> v;
-        v.put(x);
-        __builtin_memcpy(p + e, v.w, 16);
+        vec_any y;
+        __builtin_memcpy(&y, v.w, 16);
+        if (NT)
+            __builtin_nontemporal_store(y, (vec_any *)(p + e));
+        else
+            *(vec_any *)(p + e) = y;
     } else {
-#pragma unroll
-        for (uint32_t i = 0; i < VEC; ++i)
-            if (e + i < n) p[e + i] = num_round<TYPE>(x[i]);
+#pragma unroll 1
+        for (; e < n; ++e) p[e] = v.pop();
     }
 }
 
@@ -199,6 +277,22 @@ __device__ __forceinline__ uint32_t load_index(const void *p, uint64_t i, uint32
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// exp((x - m) / t) as 2^(x c - R) times 2^(R - m c), c = log2(e) / t and R the
+// whole number next to m c: one fused operation per number, whose only
+// rounding is that of a small result, and the second factor once.  R = 0 where
+// m c is no ordinary number; such sums come out of range and are formed again
+// from x - m.
+struct Base2 {
+    float c, r;
+    __device__ __forceinline__ Base2(float m, float c_) : c(c_) {
+        const float x = rintf(m * c_);
+        r = fabsf(x) < 1e30f ? x : 0.f;
+    }
+    __device__ __forceinline__ float operator()(float x) const { return exp2_fast(fmaf(x, c, -r)); }
+    __device__ __forceinline__ float to(float m) const { return exp2_fast(-fmaf(m, c, -r)); }
+};
+__device__ __forceinline__ bool sum_in_range(float s) { return s > 0.25f && s < 1e30f; }
 
 // ln of a sum: the exponent apart, so that the logarithm's own error stays
 // below 1e-7 however large the sum is

@@ -2,10 +2,10 @@
 // sum of exponentials over all others.
 //
 // A block holds one slice of a row in registers.  Its first look gives every
-// thread's largest logit; the ceil(K / 8)-th largest of them in each of the
-// eight waves bounds the slice's K-th largest logit from below, and the
-// smallest of the eight bounds serves all: at least K logits reach it, and
-// with numbers in no order only about 1.5 K do.  The second look lists those
+// thread's largest logit.  Each of the eight waves offers the ceil(K / 8)-th
+// largest of its 64, and the largest offer that K threads reach bounds the
+// slice's K-th largest logit from below; with numbers in no order only little
+// more than K logits reach it.  The second look lists those
 // in LDS and adds the exponentials of the others, so no sum is ever taken off
 // another one.  A listed logit's rank is the number of listed ones before it
 // (by value, then column), counted by one thread each; ranks from K on return
@@ -66,7 +66,8 @@ __device__ __forceinline__ uint32_t wave_nth16(uint32_t key, uint32_t n) {
 struct TopShared {
     uint64_t cand[CAND], sorted[CAND];
     uint32_t count;
-    uint32_t bound[NW];
+    uint32_t bound[NW], reached[NW];
+    uint32_t rank[CAND];
     uint32_t scan[NW + 1];
     uint32_t bits[32];
     float red[3][NW];
@@ -226,45 +227,65 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
     const uint64_t avail = row_avail(a.m, row) - start;
     const SliceView<TYPE> sl = {p, avail, start, n};
     Vec<TYPE> v[NV];
+    load_slice<TYPE, NT>(v, p, n, avail);
+    if (threadIdx.x < NW) sh.reached[threadIdx.x] = 0;
+    if (threadIdx.x == NW) sh.count = 0;
+    uint32_t bits = Vec<TYPE>::max_bits_none();
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = load_vec<TYPE>(p, (i * NT + threadIdx.x) * VEC, n, avail);
-    if (threadIdx.x == 0) sh.count = 0;
-    float mx = F_NEG_INF;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) mx = fmaxf(mx, v[i].max());
-    const uint32_t nth = wave_nth16(order_key(mx) >> 16, (a.k + NW - 1) / NW);
-    if ((threadIdx.x & 63u) == 0) sh.bound[threadIdx.x >> 6] = nth;
+    for (int i = 0; i < NV; ++i) bits = v[i].max_bits(bits);
+    // every wave's nth largest, then the largest of them that K threads reach
+    const uint32_t key16 = order_key(Vec<TYPE>::max_value(bits)) >> 16, w = threadIdx.x >> 6;
+    const uint32_t full = min(NW, n / (64 * VEC)), nth = full ? (a.k + full - 1) / full : 64u;
+    const uint32_t own = wave_nth16(key16, min(nth, 64u));
+    if ((threadIdx.x & 63u) == 0) sh.bound[w] = own;
     lds_barrier();
-    uint32_t low = sh.bound[0];
+    uint32_t reached = 0;
 #pragma unroll
-    for (uint32_t i = 1; i < NW; ++i) low = min(low, sh.bound[i]);
-    float bound = key16_floor(low);
-    // list what reaches the bound, add the others' exponentials relative to it
+    for (uint32_t i = 0; i < NW; ++i) {
+        const uint32_t c = popc64(ballot(key16 >= sh.bound[i]));
+        reached = (threadIdx.x & 63u) == i ? c : reached;
+    }
+    if ((threadIdx.x & 63u) < NW) atomicAdd(&sh.reached[threadIdx.x & 63u], reached);
+    lds_barrier();
+    uint32_t low = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < NW; ++i)
+        if (sh.reached[i] >= a.k) low = max(low, sh.bound[i]);
+    float bound = low ? key16_floor(low) : F_LOWEST;
+    // mark what reaches the bound, add the others' exponentials
+    const Base2 to2(bound, a.c);
     float ref = bound, sum = 0.f;
+    uint64_t reach = 0;  // of the thread's vectors, number i VEC + e
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        v[i].keep_packed();
 #pragma unroll
         for (uint32_t e = 0; e < VEC; ++e) {
             float x = v[i].get(e);
             if (!(x < bound)) {
-                const uint32_t at = atomicAdd(&sh.count, 1u);
-                if (at < CAND) sh.cand[at] = top_key(x, start + (i * NT + threadIdx.x) * VEC + e);
+                asm volatile("");  // a branch, which most waves pass over
+                reach |= 1ull << (i * VEC + e);
                 x = F_NEG_INF;
             }
-            sum += exp2_fast((x - ref) * a.c);
+            sum += to2(x);
         }
+    }
+    while (reach) {
+        const uint32_t bit = __ffsll((unsigned long long)reach) - 1u;
+        reach &= reach - 1;
+        const uint32_t j = (bit / VEC * NT + threadIdx.x) * VEC + bit % VEC, at = atomicAdd(&sh.count, 1u);
+        if (at >= CAND) break;
+        sh.cand[at] = top_key(num_float<TYPE>(p[j]), start + j);
     }
     __syncthreads();
     uint32_t count = sh.count, equal = 0;
-    sum = block_sum_f<NT>(sum, sh.red[0]);
+    sum = block_sum_f<NT>(sum, sh.red[0]) * to2.to(bound);
     const bool exact = count > CAND;
     if (exact) {
         bound = top_exact<TYPE>(sl, a.k, sh, &equal);
         count = sh.count;
     }
     // other logits than these are listed, or all that was added lies far below the bound
-    if (exact || !(sum > 1e-30f)) {
+    if (exact || !(sum > 1e-20f && sum < 1e30f)) {
         const float2 x = sum_below<TYPE>(sl, bound, a.c, sh.red + 1);
         ref = x.x;
         sum = x.y;
@@ -274,64 +295,88 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
         }
         __syncthreads();
     }
-    // ranks
-    for (uint32_t i = threadIdx.x; i < count; i += NT) {
-        const uint64_t key = sh.cand[i];
-        uint32_t rank = 0;
-        for (uint32_t j = 0; j < count; ++j) rank += sh.cand[j] > key ? 1u : 0u;
-        sh.sorted[rank] = key;
+    // ranks: each listed logit's count of those before it, shared by threads where they are few
+    const uint32_t lanes = (count + 63u) & ~63u, ways = lanes && lanes < NT ? NT / lanes : 1u;
+    for (uint32_t i = threadIdx.x; i < count; i += NT) sh.rank[i] = 0;
+    __syncthreads();
+    if (threadIdx.x < ways * lanes) {
+        const uint32_t way = threadIdx.x / lanes;
+        for (uint32_t i = threadIdx.x % lanes; i < count; i += NT) {
+            const uint64_t key = sh.cand[i];
+            uint32_t rank = 0;
+            for (uint32_t j = way; j < count; j += ways) rank += sh.cand[j] > key ? 1u : 0u;
+            if (rank) atomicAdd(&sh.rank[i], rank);
+        }
     }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < count; i += NT) sh.sorted[sh.rank[i]] = sh.cand[i];
     __syncthreads();
     top_finish(a, row, (uint64_t)blockIdx.x, sh.sorted, count, ref, sum, sh.red[1]);
 }
 
-// `fan` sorted lists of a row into one.  An entry's rank is its place in its
-// own list and, by binary search, the entries of every other list before it.
+// `fan` sorted lists of a row into one.  Of F full lists the ceil(K / F)-th
+// entries bound the K-th largest of all from below, as the threads' largest do
+// in a slice: only what reaches the smallest of them is ranked.
 constexpr uint32_t JT = 256;
 __global__ __launch_bounds__(JT) void k_top_join(TopArgs a) {
     __shared__ uint64_t in[TOP_JOIN], sorted[TOP_JOIN];
-    __shared__ float red[JT / 64];
+    __shared__ float red[3][JT / 64];
+    __shared__ uint32_t full, entries;
+    __shared__ uint64_t bound;
     const uint32_t groups = (a.lists_in + a.fan - 1) / a.fan, K = a.k;
     const uint64_t row = blockIdx.x / groups;
     const uint32_t first = blockIdx.x % groups * a.fan, lists = min(a.fan, a.lists_in - first);
     const uint64_t from = row * a.lists_in + first;
-    for (uint32_t i = threadIdx.x; i < lists * K; i += JT) in[i] = a.keys_in[from * K + i];
-    float ref = F_NEG_INF, sum = 0.f;
-    for (uint32_t i = 0; i < lists; ++i)
-        if (a.sums_in[from + i].y > 0.f) ref = fmaxf(ref, a.sums_in[from + i].x);
-    for (uint32_t i = 0; i < lists; ++i) {
+    if (threadIdx.x == 0) full = entries = 0, bound = ~0ull;
+    for (uint32_t i = threadIdx.x; i < lists * K; i += JT) sorted[i] = a.keys_in[from * K + i];
+    float ref = F_NEG_INF;
+    for (uint32_t i = threadIdx.x; i < lists; i += JT) {
+        const float2 x = a.sums_in[from + i];
+        if (x.y > 0.f) ref = fmaxf(ref, x.x);
+    }
+    ref = block_max_f<JT>(ref, red[0]);
+    float sum = 0.f;
+    for (uint32_t i = threadIdx.x; i < lists; i += JT) {
         const float2 x = a.sums_in[from + i];
         sum += top_rescale(x.y, x.x, ref, a.c);
     }
+    sum = block_sum_f<JT>(sum, red[1]);
     __syncthreads();
-    uint32_t total = 0;
-    for (uint32_t i = threadIdx.x; i < lists * K; i += JT) {
-        const uint64_t key = in[i];
-        if (!key) continue;
-        const uint32_t own = i / K;
-        uint32_t rank = i - own * K;
-        for (uint32_t l = 0; l < lists; ++l) {
-            if (l == own) continue;
-            uint32_t lo = 0, hi = K;  // entries of list l above the key
-            while (lo < hi) {
-                const uint32_t mid = (lo + hi) / 2;
-                if (in[l * K + mid] > key)
-                    lo = mid + 1;
-                else
-                    hi = mid;
-            }
-            rank += lo;
-        }
-        sorted[rank] = key;
-        ++total;
+    for (uint32_t i = threadIdx.x; i < lists; i += JT)
+        if (sorted[i * K + K - 1]) atomicAdd(&full, 1u);
+    __syncthreads();
+    const uint32_t nth = full ? (K + full - 1) / full : 0;
+    for (uint32_t i = threadIdx.x; nth && i < lists; i += JT)
+        if (sorted[i * K + K - 1]) atomicMin((unsigned long long *)&bound, sorted[i * K + nth - 1]);
+    __syncthreads();
+    const uint64_t least = nth ? bound : 1;
+    float left = 0.f;  // what does not reach the bound returns to the sum, relative to the bound
+    const float least_x = key_value(least);
+    const uint32_t rounds = (lists * K + JT - 1) / JT;
+    for (uint32_t r = 0; r < rounds; ++r) {
+        const uint32_t i = r * JT + threadIdx.x;
+        const uint64_t key = i < lists * K ? sorted[i] : 0;
+        if (key >= least)
+            in[atomicAdd(&entries, 1u)] = key;
+        else if (key)
+            left += exp2_fast((key_value(key) - least_x) * a.c);
     }
-    __shared__ uint32_t entries;
-    if (threadIdx.x == 0) entries = 0;
     __syncthreads();
-    total = wave_sum(total);
-    if ((threadIdx.x & 63u) == 0 && total) atomicAdd(&entries, total);
+    const uint32_t n = entries;
+    left = block_sum_f<JT>(left, red[2]);
+    if (left > 0.f) {
+        const float b = fmaxf(ref, least_x);
+        sum = top_rescale(sum, ref, b, a.c) + top_rescale(left, least_x, b, a.c);
+        ref = b;
+    }
+    for (uint32_t i = threadIdx.x; i < n; i += JT) {
+        const uint64_t key = in[i];
+        uint32_t rank = 0;
+        for (uint32_t j = 0; j < n; ++j) rank += in[j] > key ? 1u : 0u;
+        sorted[rank] = key;
+    }
     __syncthreads();
-    top_finish(a, row, (uint64_t)blockIdx.x, sorted, entries, ref, sum, red);
+    top_finish(a, row, (uint64_t)blockIdx.x, sorted, n, ref, sum, red[0]);
 }
 
 template <uint32_t TYPE>
