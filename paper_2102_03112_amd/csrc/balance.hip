@@ -22,11 +22,11 @@ struct BalanceArgs {
     Routes r;
     uint32_t parts, part_rows;  // blocks per group, rows per block (but the last)
     float coef;
-    // groups of several blocks, per block: sums of probabilities and choices (E each), valid rows
-    float *psum;
-    uint32_t *pcount, *prows;
-    double *gloss;     // per group: sum_e f P
-    uint32_t *done;    // groups joined so far
+    // groups of several blocks: (sum of probabilities, choices) per block and expert, valid rows per block
+    uint2 *partial;
+    uint32_t *prows;
+    uint32_t col_blocks;  // joining blocks per group
+    double *gloss;        // sum_e f P per group, or per joining block
     int32_t *counts_out, *rows_out;
     float *prob_out, *loss_out;
     // backward
@@ -35,19 +35,6 @@ struct BalanceArgs {
     void *grad;
     uint64_t grad_stride;
 };
-
-template <uint32_t LANES>
-__device__ __forceinline__ float lanes_max(float v) {
-#pragma unroll
-    for (uint32_t o = 1; o < LANES; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
-}
-template <uint32_t LANES>
-__device__ __forceinline__ float lanes_sum(float v) {
-#pragma unroll
-    for (uint32_t o = 1; o < LANES; o <<= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
 
 // x := softmax of the row that the LANES lanes share; 0 where all is -inf
 template <uint32_t LANES, uint32_t N>
@@ -64,7 +51,7 @@ __device__ __forceinline__ void row_softmax(float (&x)[N]) {
         s += x[i];
     }
     s = lanes_sum<LANES>(s);
-    const float inv = s == 0.f ? 0.f : 1.f / s;
+    const float inv = s == 0.f ? 0.f : __builtin_amdgcn_rcpf(s);  // within 1 ulp
 #pragma unroll
     for (uint32_t i = 0; i < N; ++i) x[i] *= inv;
 }
@@ -83,23 +70,41 @@ __device__ __forceinline__ Rows block_rows(const BalanceArgs &a) {
     return b;
 }
 
-// One row's columns of this lane: NI vectors, lane-contiguous per vector.
-template <uint32_t TYPE, uint32_t LANES, uint32_t NI>
-__device__ __forceinline__ void load_row(const Matrix &m, uint64_t row, bool valid, uint32_t sub,
-                                         float (&x)[NI * Num<TYPE>::VEC]) {
-    constexpr uint32_t VEC = Num<TYPE>::VEC;
+// A lane's columns of U rows, `apart` rows from one to the next: NI vectors a
+// row.  All are loaded before any is used.
+template <uint32_t TYPE, uint32_t LANES, uint32_t NI, uint32_t U>
+struct RowBatch {
+    static constexpr uint32_t VEC = Num<TYPE>::VEC;
+    Vec<TYPE> v[U][NI];
+    bool valid[U];
+
+    __device__ __forceinline__ void load(const BalanceArgs &a, uint64_t row, uint64_t end, uint32_t apart,
+                                         uint32_t sub) {
 #pragma unroll
-    for (uint32_t i = 0; i < NI; ++i) {
-        Vec<TYPE> v;
-        if (valid)
-            v = load_vec<TYPE, false>((const typename Num<TYPE>::T *)m.p + row * m.stride, (i * LANES + sub) * VEC, m.cols,
-                               row_avail(m, row));
-        else
-            v.fill_neg_inf();
+        for (uint32_t u = 0; u < U; ++u) {
+            const uint64_t r = row + u * apart;
+            valid[u] = r < end && (!a.r.mask || a.r.mask[r]);
+        }
 #pragma unroll
-        for (uint32_t e = 0; e < VEC; ++e) x[i * VEC + e] = v.get(e);
+        for (uint32_t u = 0; u < U; ++u) {
+            const uint64_t r = row + u * apart;
+#pragma unroll
+            for (uint32_t i = 0; i < NI; ++i) {
+                v[u][i].fill_neg_inf();
+                if (valid[u])
+                    v[u][i] = load_vec<TYPE, false>((const typename Num<TYPE>::T *)a.m.p + r * a.m.stride,
+                                                    (i * LANES + sub) * VEC, a.m.cols, row_avail(a.m, r));
+            }
+        }
     }
-}
+    __device__ __forceinline__ void get(uint32_t u, float (&x)[NI * VEC]) const {
+#pragma unroll
+        for (uint32_t i = 0; i < NI * VEC; ++i) x[i] = v[u][i / VEC].get(i % VEC);
+    }
+};
+// rows a lane holds at once: 16 to 64 registers
+template <uint32_t NI>
+constexpr uint32_t ROWS_AT_ONCE = NI == 1 ? 4 : 2;
 
 // One expert's outputs at place i = group E + e; adds count P to the loss.
 __device__ __forceinline__ void put_column(const BalanceArgs &a, uint64_t i, uint32_t count, double p, double &loss) {
@@ -109,47 +114,47 @@ __device__ __forceinline__ void put_column(const BalanceArgs &a, uint64_t i, uin
 }
 
 // The block's sum of the threads' losses (valid on thread 0).
+template <uint32_t THREADS>
 __device__ __forceinline__ double block_loss(double loss, double *red) {
     loss = wave_sum_f64(loss);
     if ((threadIdx.x & 63u) == 0) red[threadIdx.x >> 6] = loss;
     __syncthreads();
-    for (uint32_t i = 1; threadIdx.x == 0 && i < BW; ++i) loss += red[i];
+    for (uint32_t i = 1; threadIdx.x == 0 && i < THREADS / 64; ++i) loss += red[i];
     return loss;
 }
 
-// A group's outputs from sum_e count P (f = E count / (k n)); the only group's
-// loss is the call's.
-__device__ __forceinline__ void put_group(const BalanceArgs &a, uint32_t g, uint32_t n, double loss) {
-    loss *= n ? (double)a.m.cols / ((double)a.r.k * n) : 0.0;
-    a.rows_out[g] = (int32_t)n;
-    if (a.r.groups == 1)
-        a.loss_out[0] = (float)(a.coef * loss);
-    else
-        __hip_atomic_store(&a.gloss[g], loss, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// sum_e f P from sum_e count P, with f = E count / (k n)
+__device__ __forceinline__ double group_factor(const BalanceArgs &a, uint32_t n) {
+    return n ? (double)a.m.cols / ((double)a.r.k * n) : 0.0;
 }
 
 template <uint32_t TYPE, uint32_t LANES, uint32_t NI>
 __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
     constexpr uint32_t VEC = Num<TYPE>::VEC, N = NI * VEC, RPW = 64 / LANES, COLS = LANES * N;
+    constexpr uint32_t U = ROWS_AT_ONCE<NI>;
     __shared__ float sums[BW][COLS];
     __shared__ uint32_t hist[MAX_EXPERTS];
     __shared__ uint32_t rows;
     __shared__ double red[BW];
     const uint32_t E = a.m.cols, lane = threadIdx.x & 63u, w = threadIdx.x >> 6, sub = lane % LANES;
     const Rows b = block_rows(a);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;
     for (uint32_t e = threadIdx.x; e < E; e += BT) hist[e] = 0;
     if (threadIdx.x == 0) rows = 0;
     float acc[N] = {};
     uint32_t n = 0;
-    for (uint64_t r = b.first + w * RPW + lane / LANES; r - lane / LANES < b.end; r += BW * RPW) {
-        const bool valid = r < b.end && (!a.r.mask || a.r.mask[r]);
-        n += valid && sub == 0;
-        float x[N];
-        load_row<TYPE, LANES, NI>(a.m, r, valid, sub, x);
-        row_softmax<LANES>(x);
+    for (uint64_t r = b.first + w * RPW + lane / LANES; r - lane / LANES < b.end; r += U * BW * RPW) {
+        RowBatch<TYPE, LANES, NI, U> rows_now;
+        rows_now.load(a, r, b.end, BW * RPW, sub);
 #pragma unroll
-        for (uint32_t i = 0; i < N; ++i) acc[i] += x[i];
+        for (uint32_t u = 0; u < U; ++u) {
+            if (r - lane / LANES + u * BW * RPW >= b.end) break;
+            n += rows_now.valid[u] && sub == 0;
+            float x[N];
+            rows_now.get(u, x);
+            row_softmax<LANES>(x);
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i) acc[i] += x[i];
+        }
     }
 #pragma unroll
     for (uint32_t i = 0; i < N; ++i) {  // the wave's rows
@@ -179,8 +184,7 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
 #pragma unroll
         for (uint32_t i = 1; i < BW; ++i) s += sums[i][e];
         if (a.parts > 1) {
-            a.psum[at + e] = s;
-            a.pcount[at + e] = hist[e];
+            a.partial[at + e] = make_uint2(__float_as_uint(s), hist[e]);
         } else {
             put_column(a, at + e, hist[e], s * inv, loss);
         }
@@ -189,85 +193,80 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
         if (threadIdx.x == 0) a.prows[blockIdx.x] = rows;
         return;
     }
-    loss = block_loss(loss, red);
-    if (threadIdx.x == 0) put_group(a, b.group, rows, loss);
+    loss = block_loss<BT>(loss, red);
+    if (threadIdx.x == 0) {
+        loss *= group_factor(a, rows);
+        a.rows_out[b.group] = (int32_t)rows;
+        if (a.r.groups == 1)
+            a.loss_out[0] = (float)(a.coef * loss);
+        else
+            a.gloss[b.group] = loss;
+    }
 }
 
-// The mean of the groups' losses, by one block.
-__device__ __forceinline__ void put_mean(const BalanceArgs &a, double *red) {
-    double s = 0.0;
-    for (uint32_t i = threadIdx.x; i < a.r.groups; i += BT)
-        s += __hip_atomic_load(&a.gloss[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    s = block_loss(s, red);
-    if (threadIdx.x == 0) a.loss_out[0] = a.r.groups ? (float)(a.coef / (double)a.r.groups * s) : 0.f;
-}
-
-__global__ __launch_bounds__(BT) void k_balance_mean(BalanceArgs a) {
-    __shared__ double red[BW];
-    put_mean(a, red);
-}
-
-// Groups of several blocks: one block joins each, and the last one to finish
-// adds the groups' losses in their order.
-__global__ __launch_bounds__(BT) void k_balance_join(BalanceArgs a) {
-    __shared__ double sums[BT];
-    __shared__ uint32_t counts[BT];
+// Groups of several blocks: joined JOIN_COLS columns a block, so that the
+// partial sums of a large batch (1024 blocks x 256 experts: 2 MiB) are read by
+// many; every block counts the group's rows for itself.
+constexpr uint32_t JT = 512, JOIN_COLS = 16, JOIN_WAYS = JT / JOIN_COLS;
+__global__ __launch_bounds__(JT) void k_balance_join(BalanceArgs a) {
+    __shared__ double sums[JOIN_WAYS][JOIN_COLS];
+    __shared__ uint32_t counts[JOIN_WAYS][JOIN_COLS];
     __shared__ uint32_t rows;
-    __shared__ double red[BW], mean_red[BW];
-    __shared__ bool last;
-    const uint32_t E = a.m.cols, g = blockIdx.x;
+    __shared__ double red[JT / 64];
+    const uint32_t E = a.m.cols, way = threadIdx.x / JOIN_COLS, col = threadIdx.x % JOIN_COLS;
+    const uint32_t g = blockIdx.x / a.col_blocks, e = blockIdx.x % a.col_blocks * JOIN_COLS + col;
     const uint64_t b0 = (uint64_t)g * a.parts;
     if (threadIdx.x == 0) rows = 0;
+    double s = 0.0;
+    uint32_t c = 0, n = 0;
+    for (uint32_t i = threadIdx.x; i < a.parts; i += JT) n += a.prows[b0 + i];
+    if (e < E) {
+#pragma unroll 4
+        for (uint32_t i = way; i < a.parts; i += JOIN_WAYS) {
+            const uint2 x = a.partial[(b0 + i) * E + e];
+            s += __uint_as_float(x.x);
+            c += x.y;
+        }
+    }
+    sums[way][col] = s;
+    counts[way][col] = c;
     __syncthreads();
-    uint32_t n = 0;
-    for (uint32_t i = threadIdx.x; i < a.parts; i += BT) n += a.prows[b0 + i];
     n = wave_sum(n);
     if ((threadIdx.x & 63u) == 0 && n) atomicAdd(&rows, n);
     __syncthreads();
     n = rows;
-    const double inv = n ? 1.0 / n : 0.0;
-    // `width` columns at a time, the blocks' sums shared by BT / width threads
-    uint32_t width = 1;
-    while (width < E && width < BT) width *= 2;
-    const uint32_t ways = BT / width, way = threadIdx.x / width;
     double loss = 0.0;
-    for (uint32_t e0 = 0; e0 < E; e0 += width) {
-        const uint32_t e = e0 + threadIdx.x % width;
-        double s = 0.0;
-        uint32_t c = 0;
-        if (e < E) {
-            for (uint32_t i = way; i < a.parts; i += ways) {
-                s += a.psum[(b0 + i) * E + e];
-                c += a.pcount[(b0 + i) * E + e];
-            }
+    if (way == 0) {
+        for (uint32_t i = 1; i < JOIN_WAYS; ++i) {
+            s += sums[i][col];
+            c += counts[i][col];
         }
-        sums[threadIdx.x] = s;
-        counts[threadIdx.x] = c;
-        __syncthreads();
-        if (way == 0 && e < E) {
-            for (uint32_t i = 1; i < ways; ++i) {
-                s += sums[threadIdx.x + i * width];
-                c += counts[threadIdx.x + i * width];
-            }
-            put_column(a, (uint64_t)g * E + e, c, s * inv, loss);
-        }
-        __syncthreads();
+        if (e < E) put_column(a, (uint64_t)g * E + e, c, n ? s / n : 0.0, loss);
     }
-    loss = block_loss(loss, red);
+    loss = block_loss<JT>(loss, red);
     if (threadIdx.x == 0) {
-        put_group(a, g, n, loss);
-        last = a.r.groups > 1 &&
-               __hip_atomic_fetch_add(a.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == a.r.groups - 1;
+        if (blockIdx.x % a.col_blocks == 0) a.rows_out[g] = (int32_t)n;
+        loss *= group_factor(a, n);
+        if (gridDim.x == 1)
+            a.loss_out[0] = (float)(a.coef * loss);
+        else
+            a.gloss[blockIdx.x] = loss;
     }
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    put_mean(a, mean_red);
+}
+
+// The mean over groups, from n parts of their losses.
+__global__ __launch_bounds__(BT) void k_balance_mean(BalanceArgs a, uint32_t n) {
+    __shared__ double red[BW];
+    double s = 0.0;
+    for (uint32_t i = threadIdx.x; i < n; i += BT) s += a.gloss[i];
+    s = block_loss<BT>(s, red);
+    if (threadIdx.x == 0) a.loss_out[0] = a.r.groups ? (float)(a.coef / (double)a.r.groups * s) : 0.f;
 }
 
 template <uint32_t TYPE, uint32_t LANES, uint32_t NI>
 __global__ __launch_bounds__(BT) void k_balance_grad(BalanceArgs a) {
     constexpr uint32_t VEC = Num<TYPE>::VEC, N = NI * VEC, RPW = 64 / LANES;
+    constexpr uint32_t U = ROWS_AT_ONCE<NI>;
     using T = typename Num<TYPE>::T;
     const uint32_t E = a.m.cols, lane = threadIdx.x & 63u, w = threadIdx.x >> 6, sub = lane % LANES;
     const Rows b = block_rows(a);
@@ -281,26 +280,34 @@ __global__ __launch_bounds__(BT) void k_balance_grad(BalanceArgs a) {
         const uint32_t e = (i / VEC * LANES + sub) * VEC + i % VEC;
         f[i] = e < E ? a.counts[(uint64_t)b.group * E + e] * per : 0.f;
     }
-    for (uint64_t r = b.first + w * RPW + lane / LANES; r - lane / LANES < b.end; r += BW * RPW) {
-        const bool there = r < b.end, valid = there && (!a.r.mask || a.r.mask[r]);
-        float x[N];
-        load_row<TYPE, LANES, NI>(a.m, r, valid, sub, x);
-        row_softmax<LANES>(x);
-        float dot = 0.f;
+    for (uint64_t r0 = b.first + w * RPW + lane / LANES; r0 - lane / LANES < b.end; r0 += U * BW * RPW) {
+        RowBatch<TYPE, LANES, NI, U> rows_now;
+        rows_now.load(a, r0, b.end, BW * RPW, sub);
 #pragma unroll
-        for (uint32_t i = 0; i < N; ++i) dot += x[i] * f[i];
-        dot = lanes_sum<LANES>(dot);
+        for (uint32_t u = 0; u < U; ++u) {
+            const uint64_t r = r0 + u * BW * RPW;
+            if (r - lane / LANES >= b.end) break;
+            float x[N];
+            rows_now.get(u, x);
+            row_softmax<LANES>(x);
+            float dot = 0.f;
 #pragma unroll
-        for (uint32_t i = 0; i < N; ++i) x[i] = valid ? scale * x[i] * (f[i] - dot) : 0.f;
-        if (there) {
+            for (uint32_t i = 0; i < N; ++i) dot += x[i] * f[i];
+            dot = lanes_sum<LANES>(dot);
 #pragma unroll
-            for (uint32_t i = 0; i < NI; ++i) {
-                const uint32_t e = (i * LANES + sub) * VEC;
-                if (e < E) store_vec<TYPE, false>((T *)a.grad + r * a.grad_stride, e, E, x + i * VEC);
+            for (uint32_t i = 0; i < N; ++i) x[i] = rows_now.valid[u] ? scale * x[i] * (f[i] - dot) : 0.f;
+            if (r < b.end) {
+#pragma unroll
+                for (uint32_t i = 0; i < NI; ++i) {
+                    const uint32_t e = (i * LANES + sub) * VEC;
+                    if (e < E) store_vec<TYPE, false>((T *)a.grad + r * a.grad_stride, e, E, x + i * VEC);
+                }
             }
         }
     }
 }
+
+constexpr uint32_t MAX_PARTS = 2048;
 
 // How a type's rows lie over lanes, and the blocks that a call takes.
 struct Shape {
@@ -314,8 +321,8 @@ Shape plan_rows(uint64_t rows, uint32_t experts, uint32_t type, uint32_t group_r
     s.ni = (vecs + 63) / 64;
     const uint64_t groups = rows ? (rows + group_rows - 1) / group_rows : 0;
     const uint64_t own = std::min<uint64_t>(rows, group_rows), step = BW * (64 / s.lanes);
-    // four blocks per CU in all, but two rounds of a block's waves at least
-    uint64_t parts = std::max<uint64_t>(1, 1024 / std::max<uint64_t>(1, groups));
+    // eight blocks per CU in all, but two rounds of a block's waves at least
+    uint64_t parts = std::max<uint64_t>(1, MAX_PARTS / std::max<uint64_t>(1, groups));
     parts = std::max<uint64_t>(1, std::min(parts, own / (2 * step)));
     const uint64_t per = own ? (own + parts - 1) / parts : 1;
     s.part_rows = (uint32_t)((per + step - 1) / step * step);
@@ -374,10 +381,11 @@ BalanceArgs balance_args(const Matrix &m, const Routes &r, float coef, const Sha
 
 }  // namespace
 
-// Results are kept per block where groups have several (at most 1024 blocks
-// then), and a loss per group where there are several.
+// Results are kept per block where groups have several (at most MAX_PARTS
+// blocks then), and losses per group or per joining block.
 size_t balance_ws_bytes(uint64_t rows, uint64_t experts) {
-    return 256 + 8 * rows + 1024 * (8 * experts + 4);
+    const uint64_t joining = MAX_PARTS / 2 * ((experts + JOIN_COLS - 1) / JOIN_COLS);
+    return 8 * std::max<uint64_t>(rows, joining) + MAX_PARTS * (8 * experts + 4);
 }
 
 hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, int32_t *counts_out,
@@ -385,11 +393,10 @@ hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, 
     const Shape sh = plan_rows(m.rows, m.cols, m.type, r.group_rows);
     BalanceArgs a = balance_args(m, r, coef, sh);
     const uint64_t blocks = (uint64_t)r.groups * sh.parts;
-    a.done = (uint32_t *)ws;
-    a.gloss = (double *)(ws + 256);
-    a.psum = (float *)(a.gloss + r.groups);
-    a.pcount = (uint32_t *)(a.psum + blocks * m.cols);
-    a.prows = a.pcount + blocks * m.cols;
+    a.gloss = (double *)ws;
+    a.col_blocks = (m.cols + JOIN_COLS - 1) / JOIN_COLS;
+    a.partial = (uint2 *)(a.gloss + (sh.parts > 1 ? r.groups * a.col_blocks : r.groups));
+    a.prows = (uint32_t *)(a.partial + blocks * m.cols);
     a.counts_out = counts_out;
     a.rows_out = rows_out;
     a.prob_out = prob_out;
@@ -398,11 +405,14 @@ hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, 
         hipError_t e = rows_dispatch<false>(a, sh, s);
         if (e != hipSuccess) return e;
     }
+    uint32_t losses = r.groups;
     if (sh.parts > 1) {
-        k_balance_join<<<r.groups, BT, 0, s>>>(a);
+        losses *= a.col_blocks;
+        k_balance_join<<<losses, JT, 0, s>>>(a);
         trace_mark(s, "k_balance_join");
-    } else if (r.groups != 1) {
-        k_balance_mean<<<1, BT, 0, s>>>(a);
+    }
+    if (losses != 1) {
+        k_balance_mean<<<1, BT, 0, s>>>(a, losses);
         trace_mark(s, "k_balance_mean");
     }
     return hipGetLastError();

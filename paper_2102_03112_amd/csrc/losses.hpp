@@ -302,16 +302,42 @@ __device__ __forceinline__ double ln_sum(double x) {
     return (double)e * 0.6931471805599453 + (double)logf(f);
 }
 
-__device__ __forceinline__ float wave_max_f(float v) {
-#pragma unroll
-    for (uint32_t o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+// A value of another lane of the row of 16 (DPP control word CTRL).
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+constexpr int DPP_XOR1 = 0xb1, DPP_XOR2 = 0x4e, DPP_MIRROR8 = 0x141, DPP_MIRROR16 = 0x140;
+
+// Maximum and sum over each aligned group of LANES lanes (a power of two), on
+// every lane of it, in one order: within four lanes, then with the mirrored
+// four, eight, then with the neighbouring row and half of the wave.
+template <uint32_t LANES, typename OP>
+__device__ __forceinline__ float lanes_reduce(float v, OP op) {
+    if constexpr (LANES >= 2) v = op(v, dpp<DPP_XOR1>(v));
+    if constexpr (LANES >= 4) v = op(v, dpp<DPP_XOR2>(v));
+    if constexpr (LANES >= 8) v = op(v, dpp<DPP_MIRROR8>(v));
+    if constexpr (LANES >= 16) v = op(v, dpp<DPP_MIRROR16>(v));
+    if constexpr (LANES >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if constexpr (LANES >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
     return v;
 }
-__device__ __forceinline__ float wave_sum_f(float v) {
-#pragma unroll
-    for (uint32_t o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+template <uint32_t LANES>
+__device__ __forceinline__ float lanes_max(float v) {
+    return lanes_reduce<LANES>(v, [](float a, float b) { return max3(a, b, b); });
 }
+template <uint32_t LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+    return lanes_reduce<LANES>(v, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float wave_max_f(float v) { return lanes_max<64>(v); }
+__device__ __forceinline__ float wave_sum_f(float v) { return lanes_sum<64>(v); }
 
 // Block-wide maximum and sum; scratch holds NT / 64 words.  The sum's order is
 // fixed.  Every thread must call them; the scratch may be used again after the
