@@ -15,7 +15,9 @@ from __future__ import annotations
 
 import ctypes
 
-from .binding import DR_EINVAL, DeepReduceError, _check, _ptr, _stream, last_error
+import torch
+
+from .binding import DR_EINVAL, DR_OK, DeepReduceError, last_error
 from .binding import lib as _base_lib
 
 TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
@@ -92,26 +94,20 @@ def lib():
 
 
 # ---------------------------------------------------------------------------
-# what the C ABI cannot check
+# what the C ABI cannot check.  A small call's time on the GPU is a few
+# microseconds, so these stay at about two in all.
 # ---------------------------------------------------------------------------
 
-
-def _number_type(t, what: str) -> int:
-    import torch
-
-    types = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
-    if t.dtype not in types:
-        raise ValueError(f"{what}: float32, bfloat16 or float16 expected, got {t.dtype}")
-    return types[t.dtype]
+_NUMBER = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+_INDEX = {torch.int32: INDEX_I32, torch.int64: INDEX_I64}
+_F32, _I32 = torch.float32, torch.int32
 
 
-def _index_type(t, what: str) -> int:
-    import torch
-
-    types = {torch.int32: INDEX_I32, torch.int64: INDEX_I64}
-    if t.dtype not in types:
-        raise ValueError(f"{what}: int32 or int64 expected, got {t.dtype}")
-    return types[t.dtype]
+def _type(table, t, what: str) -> int:
+    kind = table.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"{what}: one of {', '.join(str(d) for d in table)} expected, got {t.dtype}")
+    return kind
 
 
 def _need(ok: bool, what: str):
@@ -120,46 +116,55 @@ def _need(ok: bool, what: str):
 
 
 def _row_stride(t, what: str) -> int:
-    """Numbers between row starts of a 2-D tensor whose rows are contiguous and do not overlap."""
-    _need(t.dim() == 2, f"{what}: a 2-D tensor expected")
+    """Numbers between row starts of a 2-D tensor whose rows are contiguous."""
+    if t.dim() != 2:
+        raise ValueError(f"{what}: a 2-D tensor expected")
     rows, cols = t.shape
-    _need(cols <= 1 or t.stride(1) == 1, f"{what}: rows must be contiguous")
-    return int(t.stride(0)) if rows > 1 else int(cols)
+    row, col = t.stride()
+    if col != 1 and cols > 1:
+        raise ValueError(f"{what}: rows must be contiguous")
+    return row if rows > 1 else cols
 
 
-def _scratch(ws, like):
-    import torch
-
-    _place(ws, like, "ws")
-    _need(ws.dtype == torch.uint8 and ws.is_contiguous(), "ws: contiguous bytes expected")
-
-
-def _place(t, like, what: str):
-    _need(t.device == like.device, f"{what}: on {t.device}, the logits are on {like.device}")
-
-
-def _flat(t, n: int, dtype, like, what: str):
-    """A contiguous tensor of n elements of a type, or None."""
+def _flat(t, n: int, dtype, dev: int, what: str):
+    """The address of a contiguous tensor of n elements of a type on device dev, or None for None."""
     if t is None:
-        return
-    _place(t, like, what)
-    _need(t.dtype == dtype, f"{what}: {dtype} expected, got {t.dtype}")
-    _need(t.is_contiguous() and t.numel() == n, f"{what}: {n} contiguous elements expected")
+        return None
+    if t.dtype is not dtype or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{what}: {n} contiguous elements of {dtype} on cuda:{dev} expected, got {tuple(t.shape)} of "
+                         f"{t.dtype} on {t.device}")
+    return t.data_ptr()
 
 
-def _logits(t) -> DrLogits:
-    import torch
-
-    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), "logits: on the current device expected")
+def _logits(t):
+    """(descriptor, rows, cols, device)"""
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError("logits: on the current device expected")
     stride = _row_stride(t, "logits")
-    return DrLogits(_ptr(t), t.shape[0], t.shape[1], stride, _number_type(t, "logits"))
+    rows, cols = t.shape
+    return DrLogits(t.data_ptr(), rows, cols, stride, _type(_NUMBER, t, "logits")), rows, cols, dev
 
 
-def _grad(grad, logits) -> int:
-    _need(tuple(grad.shape) == tuple(logits.shape) and grad.dtype == logits.dtype,
-          "grad_out: the logits' shape and type expected")
-    _place(grad, logits, "grad_out")
+def _grad(grad, logits, dev: int) -> int:
+    if grad.shape != logits.shape or grad.dtype is not logits.dtype or grad.get_device() != dev:
+        raise ValueError("grad_out: the logits' shape, type and device expected")
     return _row_stride(grad, "grad_out")
+
+
+def _scratch(ws, dev: int):
+    if ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError("ws: contiguous bytes on the logits' device expected")
+    return ws.data_ptr()
+
+
+def _stream(stream, dev: int):
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _check(fn: str, status: int):
+    if status != DR_OK:
+        raise DeepReduceError(fn, status, last_error())
 
 
 def workspace_bytes(rows: int, cols: int, k: int = 1) -> int:
@@ -172,8 +177,6 @@ def workspace_bytes(rows: int, cols: int, k: int = 1) -> int:
 
 def workspace(rows: int, cols: int, k: int = 1, device="cuda"):
     """A device scratch buffer of workspace_bytes(rows, cols, k) bytes."""
-    import torch
-
     n = workspace_bytes(rows, cols, k)
     ws = torch.empty(n + 256, dtype=torch.uint8, device=device)
     off = (-ws.data_ptr()) % 256
@@ -187,17 +190,11 @@ def workspace(rows: int, cols: int, k: int = 1, device="cuda"):
 
 def top_logits(logits, k: int, temperature: float, idx_out, val_out, rest_out, ws, stream=None):
     """The k largest logits of each row and the entry for the rest (dr_top_logits)."""
-    import torch
-
-    m = _logits(logits)
-    rows = logits.shape[0]
-    _flat(idx_out, rows * k, torch.int32, logits, "idx_out")
-    _flat(val_out, rows * k, torch.float32, logits, "val_out")
-    _flat(rest_out, rows, torch.float32, logits, "rest_out")
-    _scratch(ws, logits)
+    m, rows, _, dev = _logits(logits)
     _check("dr_top_logits", lib().dr_top_logits(
-        ctypes.byref(m), k, temperature, _ptr(idx_out), _ptr(val_out), _ptr(rest_out), _ptr(ws), ws.numel(),
-        _stream(stream)))
+        ctypes.byref(m), k, temperature, _flat(idx_out, rows * k, _I32, dev, "idx_out"),
+        _flat(val_out, rows * k, _F32, dev, "val_out"), _flat(rest_out, rows, _F32, dev, "rest_out"),
+        _scratch(ws, dev), ws.numel(), _stream(stream, dev)))
 
 
 class Teacher:
@@ -206,18 +203,18 @@ class Teacher:
     alive."""
 
     def __init__(self, idx, val, rest=None):
-        import torch
-
-        _need(idx.dim() == 2 and tuple(idx.shape) == tuple(val.shape), "teacher: idx and val of one 2-D shape expected")
-        _place(val, idx, "val")
-        _flat(rest, idx.shape[0], torch.float32, idx, "rest")
+        _need(idx.dim() == 2 and idx.shape == val.shape, "teacher: idx and val of one 2-D shape expected")
+        self.rows, k = idx.shape
+        self.dev = idx.get_device()
+        _need(val.get_device() == self.dev, "teacher: idx and val on one device expected")
         self.idx, self.val, self.rest = idx, val, rest
-        self.c = DrTeacher(_ptr(idx), _ptr(val), _ptr(rest), _row_stride(idx, "idx"), _row_stride(val, "val"),
-                           idx.shape[1], _index_type(idx, "idx"), _number_type(val, "val"))
+        self.c = DrTeacher(idx.data_ptr(), val.data_ptr(), _flat(rest, self.rows, _F32, self.dev, "rest"),
+                           _row_stride(idx, "idx"), _row_stride(val, "val"), k, _type(_INDEX, idx, "idx"),
+                           _type(_NUMBER, val, "val"))
 
-    def _for(self, logits):
-        _need(self.idx.shape[0] == logits.shape[0], "teacher: one row per row of logits expected")
-        _place(self.idx, logits, "teacher")
+    def _for(self, rows: int, dev: int):
+        if self.rows != rows or self.dev != dev:
+            raise ValueError("teacher: one row per row of logits, on their device, expected")
         return ctypes.byref(self.c)
 
 
@@ -228,53 +225,36 @@ class Teacher:
 
 def distill_forward(logits, teacher: Teacher, temperature: float, weight, loss_out, stats_out, ws, stream=None):
     """Per row, weight * KL(teacher || student); stats_out (rows x STATS, or None) is for distill_backward."""
-    import torch
-
-    m = _logits(logits)
-    rows = logits.shape[0]
-    _flat(weight, rows, torch.float32, logits, "weight")
-    _flat(loss_out, rows, torch.float32, logits, "loss_out")
-    _flat(stats_out, rows * STATS, torch.float32, logits, "stats_out")
-    _scratch(ws, logits)
+    m, rows, _, dev = _logits(logits)
     _check("dr_distill_forward", lib().dr_distill_forward(
-        ctypes.byref(m), teacher._for(logits), temperature, _ptr(weight), _ptr(loss_out), _ptr(stats_out), _ptr(ws),
-        ws.numel(), _stream(stream)))
+        ctypes.byref(m), teacher._for(rows, dev), temperature, _flat(weight, rows, _F32, dev, "weight"),
+        _flat(loss_out, rows, _F32, dev, "loss_out"), _flat(stats_out, rows * STATS, _F32, dev, "stats_out"),
+        _scratch(ws, dev), ws.numel(), _stream(stream, dev)))
 
 
 def distill_backward(logits, teacher: Teacher, temperature: float, weight, upstream, stats, grad_out, stream=None):
     """The gradient at the logits; upstream (the loss's gradient per row, or None for ones) may be an expanded
     scalar.  grad_out may be the logits themselves."""
-    import torch
-
-    m = _logits(logits)
-    rows = logits.shape[0]
-    stride = 0
+    m, rows, _, dev = _logits(logits)
+    up, stride = None, 0
     if upstream is not None:
-        _place(upstream, logits, "upstream")
-        _need(upstream.dtype == torch.float32 and tuple(upstream.shape) == (rows,) and (rows <= 1 or
-              upstream.stride(0) >= 0), "upstream: one float32 per row expected")
-        stride = int(upstream.stride(0)) if rows > 1 else 0
-    _flat(weight, rows, torch.float32, logits, "weight")
-    _flat(stats, rows * STATS, torch.float32, logits, "stats")
-    grad_stride = _grad(grad_out, logits)
+        if upstream.dtype is not _F32 or upstream.dim() != 1 or upstream.shape[0] != rows or \
+                upstream.get_device() != dev:
+            raise ValueError("upstream: one float32 per row on the logits' device expected")
+        up, stride = upstream.data_ptr(), upstream.stride(0) if rows > 1 else 0
     _check("dr_distill_backward", lib().dr_distill_backward(
-        ctypes.byref(m), teacher._for(logits), temperature, _ptr(weight), _ptr(upstream), stride, _ptr(stats),
-        _ptr(grad_out), grad_stride, _stream(stream)))
+        ctypes.byref(m), teacher._for(rows, dev), temperature, _flat(weight, rows, _F32, dev, "weight"), up, stride,
+        _flat(stats, rows * STATS, _F32, dev, "stats"), grad_out.data_ptr(), _grad(grad_out, logits, dev),
+        _stream(stream, dev)))
 
 
 def distill_step(logits, teacher: Teacher, temperature: float, weight, loss_out, grad_out, ws, stream=None):
     """Loss and gradient in one call; grad_out may be the logits themselves."""
-    import torch
-
-    m = _logits(logits)
-    rows = logits.shape[0]
-    _flat(weight, rows, torch.float32, logits, "weight")
-    _flat(loss_out, rows, torch.float32, logits, "loss_out")
-    grad_stride = _grad(grad_out, logits)
-    _scratch(ws, logits)
+    m, rows, _, dev = _logits(logits)
     _check("dr_distill_step", lib().dr_distill_step(
-        ctypes.byref(m), teacher._for(logits), temperature, _ptr(weight), _ptr(loss_out), _ptr(grad_out), grad_stride,
-        _ptr(ws), ws.numel(), _stream(stream)))
+        ctypes.byref(m), teacher._for(rows, dev), temperature, _flat(weight, rows, _F32, dev, "weight"),
+        _flat(loss_out, rows, _F32, dev, "loss_out"), grad_out.data_ptr(), _grad(grad_out, logits, dev),
+        _scratch(ws, dev), ws.numel(), _stream(stream, dev)))
 
 
 # ---------------------------------------------------------------------------
@@ -282,55 +262,44 @@ def distill_step(logits, teacher: Teacher, temperature: float, weight, loss_out,
 # ---------------------------------------------------------------------------
 
 
-def _mask(mask, rows: int, logits):
-    import torch
+def _mask(mask, rows: int, dev: int):
+    if mask is None:
+        return None
+    _need(mask.dtype is torch.bool or mask.dtype is torch.uint8, "row_mask: bool or uint8 expected")
+    return _flat(mask, rows, mask.dtype, dev, "row_mask")
 
-    if mask is not None:
-        _need(mask.dtype in (torch.bool, torch.uint8), "row_mask: bool or uint8 expected")
-        _flat(mask, rows, mask.dtype, logits, "row_mask")
-    return _ptr(mask)
+
+def _groups(rows: int, group_rows: int) -> int:
+    _need(group_rows >= 1, "group_rows must be at least 1")
+    return -(-rows // group_rows)
 
 
 def balance_forward(logits, experts, row_mask, group_rows: int, coef: float, counts_out, rows_out, prob_out, loss_out,
                     ws, stream=None):
     """Per group of group_rows rows: choices per expert, valid rows, mean probabilities (prob_out may be None); and the
     balance loss.  experts: rows x k chosen ones (int32 or int64), negative where dropped."""
-    import torch
-
-    m = _logits(logits)
-    rows, E = logits.shape
-    _need(experts.dim() == 2 and experts.shape[0] == rows, "experts: one row per row of logits expected")
-    _place(experts, logits, "experts")
-    _need(group_rows >= 1, "group_rows must be at least 1")
-    G = -(-rows // group_rows)
-    _flat(counts_out, G * E, torch.int32, logits, "counts_out")
-    _flat(rows_out, G, torch.int32, logits, "rows_out")
-    _flat(prob_out, G * E, torch.float32, logits, "prob_out")
-    _flat(loss_out, 1, torch.float32, logits, "loss_out")
-    _scratch(ws, logits)
-    r = DrRoutes(_ptr(experts), _row_stride(experts, "experts"), experts.shape[1], _index_type(experts, "experts"),
-                 _mask(row_mask, rows, logits), group_rows)
+    m, rows, E, dev = _logits(logits)
+    G = _groups(rows, group_rows)
+    stride = _row_stride(experts, "experts")
+    if experts.shape[0] != rows or experts.get_device() != dev:
+        raise ValueError("experts: one row per row of logits, on their device, expected")
+    r = DrRoutes(experts.data_ptr(), stride, experts.shape[1], _type(_INDEX, experts, "experts"),
+                 _mask(row_mask, rows, dev), group_rows)
     _check("dr_balance_forward", lib().dr_balance_forward(
-        ctypes.byref(m), ctypes.byref(r), coef, _ptr(counts_out), _ptr(rows_out), _ptr(prob_out), _ptr(loss_out),
-        _ptr(ws), ws.numel(), _stream(stream)))
+        ctypes.byref(m), ctypes.byref(r), coef, _flat(counts_out, G * E, _I32, dev, "counts_out"),
+        _flat(rows_out, G, _I32, dev, "rows_out"), _flat(prob_out, G * E, _F32, dev, "prob_out"),
+        _flat(loss_out, 1, _F32, dev, "loss_out"), _scratch(ws, dev), ws.numel(), _stream(stream, dev)))
 
 
 def balance_backward(logits, k: int, row_mask, group_rows: int, coef: float, counts, count_rows, rows_in, upstream,
                      grad_out, stream=None):
     """The balance loss's gradient at the router's logits.  counts and count_rows: a worker's own (count_rows is
     rows_in then) or the sums over all workers; upstream: one float32, or None for 1."""
-    import torch
-
-    m = _logits(logits)
-    rows, E = logits.shape
-    _need(group_rows >= 1, "group_rows must be at least 1")
-    G = -(-rows // group_rows)
-    _flat(counts, G * E, torch.int32, logits, "counts")
-    _flat(count_rows, G, torch.int32, logits, "count_rows")
-    _flat(rows_in, G, torch.int32, logits, "rows_in")
-    _flat(upstream, 1, torch.float32, logits, "upstream")
-    grad_stride = _grad(grad_out, logits)
-    r = DrRoutes(None, 0, k, INDEX_I32, _mask(row_mask, rows, logits), group_rows)
+    m, rows, E, dev = _logits(logits)
+    G = _groups(rows, group_rows)
+    r = DrRoutes(None, 0, k, INDEX_I32, _mask(row_mask, rows, dev), group_rows)
     _check("dr_balance_backward", lib().dr_balance_backward(
-        ctypes.byref(m), ctypes.byref(r), coef, _ptr(counts), _ptr(count_rows), _ptr(rows_in), _ptr(upstream),
-        _ptr(grad_out), grad_stride, _stream(stream)))
+        ctypes.byref(m), ctypes.byref(r), coef, _flat(counts, G * E, _I32, dev, "counts"),
+        _flat(count_rows, G, _I32, dev, "count_rows"), _flat(rows_in, G, _I32, dev, "rows_in"),
+        _flat(upstream, 1, _F32, dev, "upstream"), grad_out.data_ptr(), _grad(grad_out, logits, dev),
+        _stream(stream, dev)))
