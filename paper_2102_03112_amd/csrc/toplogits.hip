@@ -22,6 +22,9 @@ namespace {
 
 constexpr uint32_t NT = TOP_THREADS, NW = NT / 64;
 constexpr uint32_t CAND = 1024;  // listed logits per slice: four times the largest K
+// room for what one wave lists: all that it holds, or eight times an even share of the largest K
+template <int NV>
+constexpr uint32_t WAVE_CAND = NV == 1 ? 512 : 256;
 
 // One row's payload, or one list of a join: `keys` hold the value's order key
 // above the complement of the column, so a larger key comes first and no two
@@ -65,9 +68,9 @@ __device__ __forceinline__ uint32_t wave_nth16(uint32_t key, uint32_t n) {
 
 struct TopShared {
     uint64_t cand[CAND], sorted[CAND];
-    uint32_t count;
-    uint32_t bound[NW], reached[NW];
     uint32_t rank[CAND];
+    uint32_t count;
+    uint32_t bound[NW], reached[NW], listed[NW];
     uint32_t scan[NW + 1];
     uint32_t bits[32];
     float red[3][NW];
@@ -78,29 +81,58 @@ __device__ __forceinline__ float top_rescale(float x, float a, float b, float c)
     return x == 0.f ? 0.f : x * exp2_fast((a - b) * c);
 }
 
+// sorted[] := the n keys of in[] in descending order, by counting the keys
+// before each, which the block's threads share where keys are few.
+template <uint32_t THREADS>
+__device__ __forceinline__ void rank_keys(const uint64_t *in, uint32_t n, uint32_t *rank, uint64_t *sorted) {
+    const uint32_t lanes = (n + 63u) & ~63u, ways = lanes && lanes < THREADS ? THREADS / lanes : 1u;
+    for (uint32_t i = threadIdx.x; i < n; i += THREADS) rank[i] = 0;
+    __syncthreads();
+    if (ways > 1) {
+        const uint32_t way = threadIdx.x / lanes, i = threadIdx.x % lanes;
+        if (way < ways && i < n) {
+            const uint64_t key = in[i];
+            uint32_t r = 0;
+            for (uint32_t j = way; j < n; j += ways) r += in[j] > key ? 1u : 0u;
+            atomicAdd(&rank[i], r);
+        }
+    } else {
+        for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
+            const uint64_t key = in[i];
+            uint32_t r = 0;
+            for (uint32_t j = 0; j < n; ++j) r += in[j] > key ? 1u : 0u;
+            rank[i] = r;
+        }
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < n; i += THREADS) sorted[rank[i]] = in[i];
+    __syncthreads();
+}
+
 // The end of a slice or a join: n sorted keys, and (ref, sum) of everything
 // else.  Writes the first K keys and returns the rest to the sum.
+template <uint32_t THREADS>
 __device__ __forceinline__ void top_finish(const TopArgs &a, uint64_t row, uint64_t list, const uint64_t *sorted,
                                            uint32_t n, float ref, float sum, float *red) {
     const uint32_t K = a.k;
     if (n > K) {  // sorted[K] is the largest of what returns
         const float first = key_value(sorted[K]), b = fmaxf(ref, first);
         float back = 0.f;
-        for (uint32_t i = K + threadIdx.x; i < n; i += blockDim.x)
+        for (uint32_t i = K + threadIdx.x; i < n; i += THREADS)
             back += exp2_fast((key_value(sorted[i]) - b) * a.c);
         back = wave_sum_f(back);
         if ((threadIdx.x & 63u) == 0) red[threadIdx.x >> 6] = back;
         lds_barrier();
         sum = top_rescale(sum, ref, b, a.c);
-        for (uint32_t i = 0; i < blockDim.x / 64; ++i) sum += red[i];
+        for (uint32_t i = 0; i < THREADS / 64; ++i) sum += red[i];
         ref = b;
     }
     if (a.keys) {
-        for (uint32_t i = threadIdx.x; i < K; i += blockDim.x) a.keys[list * K + i] = i < n ? sorted[i] : 0;
+        for (uint32_t i = threadIdx.x; i < K; i += THREADS) a.keys[list * K + i] = i < n ? sorted[i] : 0;
         if (threadIdx.x == 0) a.sums[list] = make_float2(ref, sum);
         return;
     }
-    for (uint32_t i = threadIdx.x; i < K; i += blockDim.x) {
+    for (uint32_t i = threadIdx.x; i < K; i += THREADS) {
         const uint64_t key = i < n ? sorted[i] : 0;
         a.idx_out[row * K + i] = i < n ? (int32_t)(0xffffffffu - (uint32_t)key) : -1;
         a.val_out[row * K + i] = i < n ? key_value(key) : F_NEG_INF;
@@ -221,6 +253,7 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
     using N = Num<TYPE>;
     constexpr uint32_t VEC = N::VEC;
     __shared__ TopShared sh;
+    __shared__ uint2 wave_cand[NW][WAVE_CAND<NV>];  // a listed logit and its column in the slice
     const uint64_t row = blockIdx.x / a.sl.n;
     const uint32_t s = blockIdx.x % a.sl.n, start = s * a.sl.len, n = min(a.sl.len, a.m.cols - start);
     const auto *p = (const typename N::T *)a.m.p + row * a.m.stride + start;
@@ -229,7 +262,6 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
     Vec<TYPE> v[NV];
     load_slice<TYPE, NT>(v, p, n, avail);
     if (threadIdx.x < NW) sh.reached[threadIdx.x] = 0;
-    if (threadIdx.x == NW) sh.count = 0;
     uint32_t bits = Vec<TYPE>::max_bits_none();
 #pragma unroll
     for (int i = 0; i < NV; ++i) bits = v[i].max_bits(bits);
@@ -252,34 +284,46 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
     for (uint32_t i = 0; i < NW; ++i)
         if (sh.reached[i] >= a.k) low = max(low, sh.bound[i]);
     float bound = low ? key16_floor(low) : F_LOWEST;
-    // mark what reaches the bound, add the others' exponentials
+    // list what reaches the bound, wave by wave, and add the others' exponentials
     const Base2 to2(bound, a.c);
     float ref = bound, sum = 0.f;
-    uint64_t reach = 0;  // of the thread's vectors, number i VEC + e
+    uint32_t listed = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
+        float x[VEC];
 #pragma unroll
         for (uint32_t e = 0; e < VEC; ++e) {
-            float x = v[i].get(e);
-            if (!(x < bound)) {
-                asm volatile("");  // a branch, which most waves pass over
-                reach |= 1ull << (i * VEC + e);
-                x = F_NEG_INF;
+            x[e] = v[i].get(e);
+            const bool reach = !(x[e] < bound);
+            if (const uint64_t any = ballot(reach)) {
+                uint32_t col = threadIdx.x * VEC;
+                asm volatile("" : "+v"(col));  // a branch, which most waves pass over, and its columns stay in it
+                const uint32_t at = listed + lanes_below(any);
+                if (reach && at < WAVE_CAND<NV>)
+                    wave_cand[w][at] = make_uint2(__float_as_uint(x[e]), col + (i * NT * VEC + e));
+                x[e] = reach ? F_NEG_INF : x[e];
+                listed += popc64(any);
             }
-            sum += to2(x);
         }
+#pragma unroll
+        for (uint32_t e = 0; e < VEC; ++e) sum += to2(x[e]);
+        asm volatile("" : "+v"(sum));  // now, not when all vectors' numbers are unpacked
     }
-    while (reach) {
-        const uint32_t bit = __ffsll((unsigned long long)reach) - 1u;
-        reach &= reach - 1;
-        const uint32_t j = (bit / VEC * NT + threadIdx.x) * VEC + bit % VEC, at = atomicAdd(&sh.count, 1u);
-        if (at >= CAND) break;
-        sh.cand[at] = top_key(num_float<TYPE>(p[j]), start + j);
-    }
+    if ((threadIdx.x & 63u) == 0) sh.listed[w] = listed;
     __syncthreads();
-    uint32_t count = sh.count, equal = 0;
+    uint32_t count = 0, before = 0, equal = 0;
+    bool exact = false;
+#pragma unroll
+    for (uint32_t i = 0; i < NW; ++i) {
+        before = i == w ? count : before;
+        count += sh.listed[i];
+        exact |= sh.listed[i] > WAVE_CAND<NV>;
+    }
+    exact |= count > CAND;
+    if (!exact)
+        for (uint32_t i = threadIdx.x & 63u; i < listed; i += 64)
+            sh.cand[before + i] = top_key(__uint_as_float(wave_cand[w][i].x), start + wave_cand[w][i].y);
     sum = block_sum_f<NT>(sum, sh.red[0]) * to2.to(bound);
-    const bool exact = count > CAND;
     if (exact) {
         bound = top_exact<TYPE>(sl, a.k, sh, &equal);
         count = sh.count;
@@ -295,31 +339,19 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
         }
         __syncthreads();
     }
-    // ranks: each listed logit's count of those before it, shared by threads where they are few
-    const uint32_t lanes = (count + 63u) & ~63u, ways = lanes && lanes < NT ? NT / lanes : 1u;
-    for (uint32_t i = threadIdx.x; i < count; i += NT) sh.rank[i] = 0;
-    __syncthreads();
-    if (threadIdx.x < ways * lanes) {
-        const uint32_t way = threadIdx.x / lanes;
-        for (uint32_t i = threadIdx.x % lanes; i < count; i += NT) {
-            const uint64_t key = sh.cand[i];
-            uint32_t rank = 0;
-            for (uint32_t j = way; j < count; j += ways) rank += sh.cand[j] > key ? 1u : 0u;
-            if (rank) atomicAdd(&sh.rank[i], rank);
-        }
-    }
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < count; i += NT) sh.sorted[sh.rank[i]] = sh.cand[i];
-    __syncthreads();
-    top_finish(a, row, (uint64_t)blockIdx.x, sh.sorted, count, ref, sum, sh.red[1]);
+    rank_keys<NT>(sh.cand, count, sh.rank, sh.sorted);
+    top_finish<NT>(a, row, (uint64_t)blockIdx.x, sh.sorted, count, ref, sum, sh.red[1]);
 }
 
-// `fan` sorted lists of a row into one.  Of F full lists the ceil(K / F)-th
-// entries bound the K-th largest of all from below, as the threads' largest do
-// in a slice: only what reaches the smallest of them is ranked.
-constexpr uint32_t JT = 256;
+// `fan` sorted lists of a row into one, of at most ENTRIES keys in all.  Of F
+// full lists the ceil(K / F)-th entries bound the K-th largest of all from
+// below, as the threads' largest do in a slice: only what reaches the smallest
+// of them is ranked.  512 keys are enough for the usual few lists, and their
+// room lets eight blocks share a CU.
+template <uint32_t JT, uint32_t ENTRIES>
 __global__ __launch_bounds__(JT) void k_top_join(TopArgs a) {
-    __shared__ uint64_t in[TOP_JOIN], sorted[TOP_JOIN];
+    __shared__ uint64_t in[ENTRIES], sorted[ENTRIES];
+    __shared__ uint32_t ranks[ENTRIES];
     __shared__ float red[3][JT / 64];
     __shared__ uint32_t full, entries;
     __shared__ uint64_t bound;
@@ -328,23 +360,24 @@ __global__ __launch_bounds__(JT) void k_top_join(TopArgs a) {
     const uint32_t first = blockIdx.x % groups * a.fan, lists = min(a.fan, a.lists_in - first);
     const uint64_t from = row * a.lists_in + first;
     if (threadIdx.x == 0) full = entries = 0, bound = ~0ull;
-    for (uint32_t i = threadIdx.x; i < lists * K; i += JT) sorted[i] = a.keys_in[from * K + i];
-    float ref = F_NEG_INF;
-    for (uint32_t i = threadIdx.x; i < lists; i += JT) {
+    const float2 mine = threadIdx.x < lists ? a.sums_in[from + threadIdx.x] : make_float2(F_NEG_INF, 0.f);
+#pragma unroll
+    for (uint32_t i = threadIdx.x; i < ENTRIES; i += JT)
+        if (i < lists * K) sorted[i] = a.keys_in[from * K + i];
+    float ref = mine.y > 0.f ? mine.x : F_NEG_INF;
+    for (uint32_t i = threadIdx.x + JT; i < lists; i += JT) {
         const float2 x = a.sums_in[from + i];
         if (x.y > 0.f) ref = fmaxf(ref, x.x);
     }
     ref = block_max_f<JT>(ref, red[0]);
-    float sum = 0.f;
-    for (uint32_t i = threadIdx.x; i < lists; i += JT) {
+    for (uint32_t i = threadIdx.x; i < lists; i += JT)
+        if (sorted[i * K + K - 1]) atomicAdd(&full, 1u);
+    float sum = top_rescale(mine.y, mine.x, ref, a.c);
+    for (uint32_t i = threadIdx.x + JT; i < lists; i += JT) {
         const float2 x = a.sums_in[from + i];
         sum += top_rescale(x.y, x.x, ref, a.c);
     }
     sum = block_sum_f<JT>(sum, red[1]);
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < lists; i += JT)
-        if (sorted[i * K + K - 1]) atomicAdd(&full, 1u);
-    __syncthreads();
     const uint32_t nth = full ? (K + full - 1) / full : 0;
     for (uint32_t i = threadIdx.x; nth && i < lists; i += JT)
         if (sorted[i * K + K - 1]) atomicMin((unsigned long long *)&bound, sorted[i * K + nth - 1]);
@@ -352,10 +385,8 @@ __global__ __launch_bounds__(JT) void k_top_join(TopArgs a) {
     const uint64_t least = nth ? bound : 1;
     float left = 0.f;  // what does not reach the bound returns to the sum, relative to the bound
     const float least_x = key_value(least);
-    const uint32_t rounds = (lists * K + JT - 1) / JT;
-    for (uint32_t r = 0; r < rounds; ++r) {
-        const uint32_t i = r * JT + threadIdx.x;
-        const uint64_t key = i < lists * K ? sorted[i] : 0;
+    for (uint32_t i = threadIdx.x; i < lists * K; i += JT) {
+        const uint64_t key = sorted[i];
         if (key >= least)
             in[atomicAdd(&entries, 1u)] = key;
         else if (key)
@@ -369,15 +400,10 @@ __global__ __launch_bounds__(JT) void k_top_join(TopArgs a) {
         sum = top_rescale(sum, ref, b, a.c) + top_rescale(left, least_x, b, a.c);
         ref = b;
     }
-    for (uint32_t i = threadIdx.x; i < n; i += JT) {
-        const uint64_t key = in[i];
-        uint32_t rank = 0;
-        for (uint32_t j = 0; j < n; ++j) rank += in[j] > key ? 1u : 0u;
-        sorted[rank] = key;
-    }
-    __syncthreads();
-    top_finish(a, row, (uint64_t)blockIdx.x, sorted, n, ref, sum, red[0]);
+    rank_keys<JT>(in, n, ranks, sorted);
+    top_finish<JT>(a, row, (uint64_t)blockIdx.x, sorted, n, ref, sum, red[0]);
 }
+constexpr uint32_t FEW_ENTRIES = 512;
 
 template <uint32_t TYPE>
 void slice_kernel(const TopArgs &a, hipStream_t s) {
@@ -442,7 +468,11 @@ hipError_t launch_top(const Matrix &m, uint32_t k, float temperature, int32_t *i
         a.fan = p.fan;
         a.keys = groups > 1 ? keys[from ^ 1] : nullptr;
         a.sums = groups > 1 ? sums[from ^ 1] : nullptr;
-        k_top_join<<<(uint32_t)(m.rows * groups), JT, 0, s>>>(a);
+        const uint32_t grid = (uint32_t)(m.rows * groups);
+        if (std::min(lists, p.fan) * k <= FEW_ENTRIES)
+            k_top_join<256, FEW_ENTRIES><<<grid, 256, 0, s>>>(a);
+        else
+            k_top_join<256, TOP_JOIN><<<grid, 256, 0, s>>>(a);
         trace_mark(s, "k_top_join");
         lists = groups;
     }
