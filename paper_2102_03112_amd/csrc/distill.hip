@@ -42,7 +42,7 @@ __device__ __forceinline__ void mark_kept(const Teacher &t, uint64_t row, uint32
     }
 }
 
-// bits of vector i (VEC of them) in the bitmap
+// bits of vector i (VEC of them) in the bitmap, in the low places
 template <uint32_t VEC>
 __device__ __forceinline__ uint32_t kept_bits(const uint32_t *bm, uint32_t i) {
     const uint32_t b = ((const uint8_t *)bm)[i * VEC / 8];
@@ -52,10 +52,10 @@ __device__ __forceinline__ uint32_t kept_bits(const uint32_t *bm, uint32_t i) {
 // (maximum, sum) of a slice's columns not kept, formed from x - m, by reading
 // the slice again: where nothing is left, where all lies near the lowest
 // number, or where a maximum of bits was no more than an estimate.
-template <uint32_t TYPE>
+template <uint32_t TYPE, uint32_t THREADS>
 __device__ __forceinline__ float2 slice_again(const typename Num<TYPE>::T *p, uint32_t n, uint64_t avail,
-                                              const uint32_t *bm, float c, float (*red)[DIST_THREADS / 64]) {
-    constexpr uint32_t VEC = Num<TYPE>::VEC, STEP = DIST_THREADS * VEC;
+                                              const uint32_t *bm, float c, float (*red)[THREADS / 64]) {
+    constexpr uint32_t VEC = Num<TYPE>::VEC, STEP = THREADS * VEC;
     float mx = F_NEG_INF, sum = 0.f;
 #pragma unroll 1
     for (uint32_t pass = 0; pass < 2; ++pass) {
@@ -74,9 +74,9 @@ __device__ __forceinline__ float2 slice_again(const typename Num<TYPE>::T *p, ui
             }
         }
         if (pass == 0)
-            mx = block_max_f<DIST_THREADS>(mx, red[0]);
+            mx = block_max_f<THREADS>(mx, red[0]);
         else
-            sum = block_sum_f<DIST_THREADS>(sum, red[1]);
+            sum = block_sum_f<THREADS>(sum, red[1]);
     }
     return make_float2(mx, sum);
 }
@@ -101,24 +101,26 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_slice(DistillArgs a) {
     uint32_t bits = Vec<TYPE>::max_bits_none();
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
+        if (i * DIST_THREADS * VEC >= n) break;
         const uint32_t b = kept_bits<VEC>(bm, i * DIST_THREADS + threadIdx.x);
-        if (b) {
-#pragma unroll
-            for (uint32_t e = 0; e < VEC; ++e)
-                if (b >> e & 1u) v[i].mask(e);
-        }
+        if (b) v[i].mask(b);
+        v[i].keep_packed();
         bits = v[i].max_bits(bits);
     }
     const float mx = block_max_f<DIST_THREADS>(Vec<TYPE>::max_value(bits), red[0]);
     const Base2 to2(mx, a.c);
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+        if (i * DIST_THREADS * VEC >= n) break;
+        v[i].keep_packed();
 #pragma unroll
         for (uint32_t e = 0; e < VEC; ++e) sum += to2(v[i].get(e));
+        asm volatile("" : "+v"(sum));  // one vector's numbers after the other
+    }
     sum = block_sum_f<DIST_THREADS>(sum, red[1]);
     float2 x = make_float2(mx, sum * to2.to(mx));
-    if (!sum_in_range(sum)) x = slice_again<TYPE>(p, n, avail, bm, a.c, red + 2);
+    if (!sum_in_range(sum)) x = slice_again<TYPE, DIST_THREADS>(p, n, avail, bm, a.c, red + 2);
     if (threadIdx.x == 0) a.part[row * a.sl.n + s] = x;
 }
 
@@ -127,42 +129,43 @@ __device__ __forceinline__ float rescale(float x, float a, float b, float c) {
     return x == 0.f ? 0.f : x * exp2_fast((a - b) * c);
 }
 
-// A row's result from its columns not kept (m_tail, tail: their maximum and
-// sum) and its kept entries, one per lane and step: student's logit x, teacher's
-// y, `there` telling whether there is one.  All lanes of a wave take part.
+// A row's result from its columns not kept (m_tail, tail: a reference at least
+// near their maximum, and their sum relative to it) and its kept entries:
+// entry(i, x, y) gives the lane's i-th of n, the student's logit x and the
+// teacher's y, or tells that there is none.  All lanes of a wave take part.
 struct RowResult {
     double loss;  // not yet times the weight
     float stats[6];
 };
-template <int NK>
-__device__ __forceinline__ RowResult row_result(float m_tail, double tail, const float (&x)[NK], const float (&y)[NK],
-                                                const bool (&there)[NK], float rest, float c, float inv_t) {
-    float m_p = rest, m = m_tail;
+template <typename ENTRY>
+__device__ __forceinline__ RowResult row_result(float m_tail, double tail, uint32_t n, ENTRY entry, float rest, float c,
+                                                float inv_t) {
+    float m_p = rest, m = m_tail, x, y;
 #pragma unroll
-    for (int i = 0; i < NK; ++i)
-        if (there[i]) {
-            m = fmaxf(m, x[i]);
-            m_p = fmaxf(m_p, y[i] * inv_t);
+    for (uint32_t i = 0; i < n; ++i)
+        if (entry(i, x, y)) {
+            m = fmaxf(m, x);
+            m_p = fmaxf(m_p, y * inv_t);
         }
     m = wave_max_f(m);
     m_p = wave_max_f(m_p);
     // sums relative to m and m_p; d: the teacher's logit less the student's
     double sum_q = 0.0, sum_p = 0.0, sum_d = 0.0;
 #pragma unroll
-    for (int i = 0; i < NK; ++i) {
-        if (!there[i]) continue;
-        if (x[i] != F_NEG_INF) sum_q += exp2_fast((x[i] - m) * c);
-        const float e = y[i] == F_NEG_INF ? 0.f : expf(y[i] * inv_t - m_p);
+    for (uint32_t i = 0; i < n; ++i) {
+        if (!entry(i, x, y)) continue;
+        if (x != F_NEG_INF) sum_q += exp2_fast((x - m) * c);
+        const float e = y == F_NEG_INF ? 0.f : exp_below(y * inv_t - m_p);
         if (e > 0.f) {
             sum_p += e;
-            sum_d += e * (((double)y[i] - (double)x[i]) * (double)inv_t);
+            sum_d += e * (((double)y - (double)x) * (double)inv_t);
         }
     }
     const double tail_q = tail == 0.0 ? 0.0 : tail * exp2_fast((m_tail - m) * c);
     sum_q = wave_sum_f64(sum_q) + tail_q;
     sum_p = wave_sum_f64(sum_p);
     sum_d = wave_sum_f64(sum_d);
-    const float e_rest = rest == F_NEG_INF ? 0.f : expf(rest - m_p);
+    const float e_rest = rest == F_NEG_INF ? 0.f : exp_below(rest - m_p);
     sum_p += e_rest;
     RowResult r;
     r.loss = 0.0;
@@ -228,7 +231,12 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_join(DistillArgs a) {
         tail += rescale(p.y, p.x, m_tail, a.c);
     }
     tail = wave_sum_f64(tail);
-    const RowResult r = row_result<NK>(m_tail, tail, x, y, there, rest, a.c, a.inv_t);
+    const auto entry = [&](uint32_t i, float &student, float &teacher) {
+        student = x[i];
+        teacher = y[i];
+        return there[i];
+    };
+    const RowResult r = row_result(m_tail, tail, NK, entry, rest, a.c, a.inv_t);
     if (lane == 0) a.loss[row] = (float)(w * r.loss);
     if (a.stats && lane < STATS) {
         float st = 0.f;
@@ -274,27 +282,188 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
         const uint32_t j = load_index(a.t.idx, row * a.t.idx_stride + k, a.t.idx_type, a.m.cols) - start;
         if (j >= n) continue;
         const float x = num_float<TYPE>(p[j]), y = load_num(a.t.val, row * a.t.val_stride + k, a.t.val_type);
-        const float e = y == F_NEG_INF ? 0.f : expf(y * a.inv_t - st[4]) * st[5];
+        const float e = y == F_NEG_INF ? 0.f : exp_below(y * a.inv_t - st[4]) * st[5];
         at[i] = j;
         g[i] = q * exp2_fast((x - m) * a.c) - scale * e;
     }
     __syncthreads();
     const Base2 to2(m_tail, a.c);
-    const bool low = fabsf(m_tail * a.c) >= 1e30f;  // all near the lowest number
     const float f2 = f * to2.to(m_tail);
+    const bool low = fabsf(m_tail * a.c) >= 1e30f;  // all near the lowest number
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const uint32_t e0 = (i * DIST_THREADS + threadIdx.x) * VEC;
+        const uint32_t s0 = i * DIST_THREADS * VEC, e0 = s0 + threadIdx.x * VEC;
+        if (s0 >= n) break;
         float x[VEC];
+        if (low) {
 #pragma unroll
-        for (uint32_t e = 0; e < VEC; ++e)
-            x[e] = low ? f * exp2_fast((v[i].get(e) - m_tail) * a.c) : f2 * to2(v[i].get(e));
-        if (e0 < n) store_vec<TYPE>(out, e0, n, x);
+            for (uint32_t e = 0; e < VEC; ++e) x[e] = f * exp2_fast((v[i].get(e) - m_tail) * a.c);
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < VEC; ++e) x[e] = f2 * to2(v[i].get(e));
+        }
+        if (s0 + DIST_THREADS * VEC <= n)
+            store_run<TYPE>(out + s0, x);
+        else if (e0 < n)
+            store_vec<TYPE>(out, e0, n, x);
     }
     __syncthreads();
 #pragma unroll
     for (uint32_t i = 0; i < PER; ++i)
         if (at[i] < n) out[at[i]] = num_round<TYPE>(g[i]);
+}
+
+// A step of one row by one block.  The row's first RES vectors of every thread
+// stay in registers from the sum to the gradient.  What a longer row has beyond
+// them is read twice, MORE vectors at a time, the second time from the cache
+// beside the memory: 256 CUs hold at most 512 rows at a time, 128 MiB of 131072
+// 16-bit numbers, and it holds 256.  A CU's blocks are rarely in one phase, so
+// that one loads and stores while another adds.  The sum is relative to the
+// largest kept logit, which is known before the row has arrived.
+constexpr int RES = 8;
+
+// Adds a run's numbers but for the kept columns, relative to a reference;
+// vector i THREADS + thread lies at bit (first + i THREADS + thread) VEC.
+template <uint32_t TYPE, uint32_t THREADS, int NV>
+__device__ __forceinline__ float sum_run(Vec<TYPE> (&v)[NV], uint32_t n, uint32_t first, const uint32_t *bm,
+                                         const Base2 &to2, float sum) {
+    constexpr uint32_t VEC = Num<TYPE>::VEC;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i * THREADS * VEC >= n) break;
+        const uint32_t b = kept_bits<VEC>(bm, first + i * THREADS + threadIdx.x);
+        if (b) v[i].mask(b);
+        v[i].keep_packed();
+#pragma unroll
+        for (uint32_t e = 0; e < VEC; ++e) sum += to2(v[i].get(e));
+        asm volatile("" : "+v"(sum));  // one vector's numbers after the other
+    }
+    return sum;
+}
+
+// Writes a run's gradients f exp2(z c - R).
+template <uint32_t TYPE, uint32_t THREADS, int NV>
+__device__ __forceinline__ void grad_run(Vec<TYPE> (&v)[NV], typename Num<TYPE>::T *out, uint32_t n, const Base2 &to2,
+                                         float f) {
+    constexpr uint32_t VEC = Num<TYPE>::VEC, STEP = THREADS * VEC;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint32_t e0 = i * STEP + threadIdx.x * VEC;
+        if (i * STEP >= n) break;
+        v[i].keep_packed();
+        float x[VEC];
+#pragma unroll
+        for (uint32_t e = 0; e < VEC; ++e) x[e] = f * to2(v[i].get(e));
+        if ((i + 1) * STEP <= n)
+            store_run<TYPE>(out + i * STEP, x);
+        else if (e0 < n)
+            store_vec<TYPE>(out, e0, n, x);
+    }
+}
+
+template <uint32_t TYPE, uint32_t THREADS>
+__global__ __launch_bounds__(THREADS, THREADS < 512 ? 8 : 6) void k_distill_row(DistillArgs a) {
+    using N = Num<TYPE>;
+    using T = typename N::T;
+    constexpr uint32_t VEC = N::VEC, STEP = THREADS * VEC, CHUNK = RES * STEP;
+    constexpr int MORE = THREADS < 512 ? 2 : 4;
+    extern __shared__ uint32_t bm[];  // a bit per column, then the kept entries:
+    const uint32_t words = (a.m.cols + 31) / 32;
+    float *const ex = (float *)(bm + words), *const ey = ex + a.t.k;  // student's logit, teacher's
+    uint32_t *const ej = (uint32_t *)(ey + a.t.k);                    // and column
+    __shared__ float red[4][THREADS / 64];
+    __shared__ float row_stats[6];
+    const uint64_t row = blockIdx.x;
+    const uint32_t n = a.m.cols;
+    T *out = (T *)a.grad + row * a.grad_stride;
+    const float w = a.weight ? a.weight[row] : 1.f;
+    if (w == 0.f) {
+        const float zero[VEC] = {};
+        for (uint32_t e = threadIdx.x * VEC; e < n; e += STEP) store_vec<TYPE>(out, e, n, zero);
+        if (threadIdx.x == 0) a.loss[row] = 0.f;
+        return;
+    }
+    const T *p = (const T *)a.m.p + row * a.m.stride;
+    const uint64_t avail = row_avail(a.m, row);
+    const uint32_t held = min(n, CHUNK);
+    Vec<TYPE> v[RES];
+    load_slice<TYPE, THREADS>(v, p, held, avail);
+    for (uint32_t i = threadIdx.x; i < words; i += THREADS) bm[i] = 0;
+    float top = F_NEG_INF;
+    for (uint32_t k = threadIdx.x; k < a.t.k; k += THREADS) {
+        const uint32_t j = load_index(a.t.idx, row * a.t.idx_stride + k, a.t.idx_type, n);
+        ej[k] = j;
+        if (j < n) {
+            ex[k] = num_float<TYPE>(p[j]);
+            ey[k] = load_num(a.t.val, row * a.t.val_stride + k, a.t.val_type);
+            top = fmaxf(top, ex[k]);
+        }
+    }
+    top = block_max_f<THREADS>(top, red[0]);
+    for (uint32_t k = threadIdx.x; k < a.t.k; k += THREADS)
+        if (ej[k] < n) atomicOr(&bm[ej[k] >> 5], 1u << (ej[k] & 31u));
+    lds_barrier();
+    float ref = top > F_NEG_INF ? top : 0.f;
+    const Base2 by_top(ref, a.c);
+    float sum = sum_run<TYPE, THREADS>(v, held, 0, bm, by_top, 0.f);
+#pragma unroll 1
+    for (uint32_t e0 = CHUNK; e0 < n; e0 += MORE * STEP) {
+        Vec<TYPE> u[MORE];
+        load_slice<TYPE, THREADS, MORE, false>(u, p + e0, n - e0, avail - e0);
+        sum = sum_run<TYPE, THREADS>(u, n - e0, e0 / VEC, bm, by_top, sum);
+    }
+    sum = block_sum_f<THREADS>(sum, red[1]);
+    float tail = sum * by_top.to(ref);
+    if (!(sum > 1e-28f && sum < 1e30f)) {
+        const float2 x = slice_again<TYPE, THREADS>(p, n, avail, bm, a.c, red + 2);
+        ref = x.x;
+        tail = x.y;
+    }
+    if (threadIdx.x < 64) {
+        const auto entry = [&](uint32_t i, float &student, float &teacher) {
+            const uint32_t k = i * 64 + threadIdx.x;
+            if (k >= a.t.k || ej[k] >= n) return false;
+            student = ex[k];
+            teacher = ey[k];
+            return true;
+        };
+        const RowResult r = row_result(ref, tail, (a.t.k + 63) / 64, entry, a.t.rest ? a.t.rest[row] : F_NEG_INF, a.c,
+                                       a.inv_t);
+        if (threadIdx.x == 0) {
+            a.loss[row] = (float)(w * r.loss);
+#pragma unroll
+            for (int i = 0; i < 6; ++i) row_stats[i] = r.stats[i];
+        }
+    }
+    lds_barrier();
+    const float m = row_stats[0] == F_NEG_INF ? 0.f : row_stats[0], scale = w * a.inv_t, q = scale * row_stats[1];
+    ref = ref == F_NEG_INF ? 0.f : ref;
+    const Base2 to2(ref, a.c);
+    const float f = scale * row_stats[3], f2 = f * to2.to(ref);
+    if (fabsf(ref * a.c) >= 1e30f) {  // all near the lowest number
+#pragma unroll 1
+        for (uint32_t e0 = threadIdx.x * VEC; e0 < n; e0 += STEP) {
+            const Vec<TYPE> u = load_vec<TYPE, false>(p, e0, n, avail);
+            float x[VEC];
+#pragma unroll
+            for (uint32_t e = 0; e < VEC; ++e) x[e] = f * exp2_fast((u.get(e) - ref) * a.c);
+            store_vec<TYPE>(out, e0, n, x);
+        }
+    } else {
+        grad_run<TYPE, THREADS>(v, out, held, to2, f2);
+#pragma unroll 1
+        for (uint32_t e0 = CHUNK; e0 < n; e0 += MORE * STEP) {
+            Vec<TYPE> u[MORE];
+            load_slice<TYPE, THREADS>(u, p + e0, n - e0, avail - e0);
+            grad_run<TYPE, THREADS>(u, out + e0, n - e0, to2, f2);
+        }
+    }
+    __syncthreads();  // the kept columns are written again
+    for (uint32_t k = threadIdx.x; k < a.t.k; k += THREADS) {
+        if (ej[k] >= n) continue;
+        const float e = ey[k] == F_NEG_INF ? 0.f : exp_below(ey[k] * a.inv_t - row_stats[4]) * row_stats[5];
+        out[ej[k]] = num_round<TYPE>(q * exp2_fast((ex[k] - m) * a.c) - scale * e);
+    }
 }
 
 Slices distill_slices(const Matrix &m) {
@@ -348,6 +517,29 @@ void grad_kernel(const DistillArgs &a, hipStream_t s) {
     trace_mark(s, "k_distill_grad");
 }
 
+// A step takes its rows one by one where they fill the chip and a row's bitmap
+// fits beside its entries.
+constexpr uint32_t ROW_MAX_COLS = 1u << 18;
+bool rows_one_by_one(const Matrix &m) { return m.rows >= 512 && m.cols <= ROW_MAX_COLS; }
+
+// Threads per row, as measured (us at 64, 128, 256, 512, 1024 threads, bfloat16):
+template <uint32_t TYPE>
+void row_kernel(const DistillArgs &a, hipStream_t s) {
+    const uint32_t grid = (uint32_t)a.m.rows, vecs = (a.m.cols + Num<TYPE>::VEC - 1) / Num<TYPE>::VEC;
+    const uint32_t lds = 4 * ((a.m.cols + 31) / 32 + 3 * a.t.k);
+    if (vecs <= 64 * RES)
+        k_distill_row<TYPE, 64><<<grid, 64, lds, s>>>(a);
+    else if (vecs <= 128 * RES)
+        k_distill_row<TYPE, 128><<<grid, 128, lds, s>>>(a);
+    else if (vecs <= 256 * RES)
+        k_distill_row<TYPE, 256><<<grid, 256, lds, s>>>(a);
+    else if (vecs <= 2 * 512 * RES)
+        k_distill_row<TYPE, 512><<<grid, 512, lds, s>>>(a);
+    else
+        k_distill_row<TYPE, 1024><<<grid, 1024, lds, s>>>(a);
+    trace_mark(s, "k_distill_row");
+}
+
 template <typename F>
 hipError_t by_type(uint32_t type, F f) {
     if (type == TYPE_F32)
@@ -395,6 +587,13 @@ hipError_t launch_distill_backward(const Matrix &m, const Teacher &t, float temp
 
 hipError_t launch_distill_step(const Matrix &m, const Teacher &t, float temperature, const float *weight,
                                float *loss_out, void *grad, uint64_t grad_stride, uint8_t *ws, hipStream_t s) {
+    if (rows_one_by_one(m)) {
+        DistillArgs a = distill_args(m, t, temperature, weight);
+        a.loss = loss_out;
+        a.grad = grad;
+        a.grad_stride = grad_stride;
+        return by_type(m.type, [&](auto type) { row_kernel<decltype(type)::value>(a, s); });
+    }
     float *stats = (float *)(ws + part_bytes(m));
     hipError_t e = launch_distill_forward(m, t, temperature, weight, loss_out, stats, ws, s);
     if (e != hipSuccess) return e;

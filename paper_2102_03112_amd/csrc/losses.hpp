@@ -102,13 +102,21 @@ struct Vec {
         else if constexpr (TYPE == TYPE_BF16)
             return __uint_as_float(i & 1 ? x & 0xffff0000u : x << 16);
         else
-            return (float)__builtin_bit_cast(half2_t, x)[i & 1];
+            return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? x >> 16 : x));
     }
-    __device__ __forceinline__ void mask(uint32_t i) {  // element i := -inf
-        if constexpr (TYPE == TYPE_F32)
-            w[i] = N::NEG_INF;
-        else
-            w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | (N::NEG_INF << 16) : (w[i / 2] & 0xffff0000u) | N::NEG_INF;
+    // elements whose bit is set := -inf (by whole words: halves of their own
+    // would take a register each)
+    __device__ __forceinline__ void mask(uint32_t bits) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            if constexpr (TYPE == TYPE_F32) {
+                w[i] = bits >> i & 1u ? N::NEG_INF : w[i];
+            } else {
+                const uint32_t lo = 0u - (bits >> (2 * i) & 1u), hi = 0u - (bits >> (2 * i + 1) & 1u);
+                const uint32_t m = (lo & 0xffffu) | (hi << 16), inf = N::NEG_INF * 0x10001u;
+                asm("v_bfi_b32 %0, %1, %2, %3" : "=v"(w[i]) : "v"(m), "v"(inf), "v"(w[i]));
+            }
+        }
     }
     // The numbers as a queue: push before the first one, take the first one off.
     __device__ __forceinline__ void push(T x) {
@@ -207,17 +215,32 @@ __device__ __forceinline__ Vec<TYPE> load_vec(const typename Num<TYPE>::T *p, ui
         v.fill_neg_inf();
     } else if (e + VEC <= avail) {
         v = load_whole<TYPE, NT>(p + e);
-        if (e + VEC > n) {
-#pragma unroll
-            for (uint32_t i = 0; i < VEC; ++i)
-                if (e + i >= n) v.mask(i);
-        }
+        if (e + VEC > n) v.mask(~0u << (n - e));
     } else {  // the matrix ends in it: number by number, the last one first
         v.fill_neg_inf();
 #pragma unroll 1
         for (uint32_t i = VEC; i-- > 0;) v.push(e + i < n ? p[e + i] : (typename Num<TYPE>::T)Num<TYPE>::NEG_INF);
     }
     return v;
+}
+
+// The calling thread's vector of a run of them that starts at p (the same on
+// every lane: the address is a scalar base and one 32-bit offset for all runs).
+template <uint32_t TYPE, bool NT>
+__device__ __forceinline__ Vec<TYPE> load_run(const typename Num<TYPE>::T *p) {
+    return load_whole<TYPE, NT>((const typename Num<TYPE>::T *)((const char *)p + threadIdx.x * 16u));
+}
+template <uint32_t TYPE, bool NT = true>
+__device__ __forceinline__ void store_run(typename Num<TYPE>::T *p, const float *x) {
+    Vec<TYPE> v;
+    v.put(x);
+    vec_any y;
+    __builtin_memcpy(&y, v.w, 16);
+    vec_any *at = (vec_any *)((char *)p + threadIdx.x * 16u);
+    if (NT)
+        __builtin_nontemporal_store(y, at);
+    else
+        *at = y;
 }
 
 // The NV vectors that a thread of a block of THREADS holds of n numbers:
@@ -228,11 +251,10 @@ __device__ __forceinline__ void load_slice(Vec<TYPE> (&v)[NV], const typename Nu
     constexpr uint32_t VEC = Num<TYPE>::VEC;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const uint32_t e = (i * THREADS + threadIdx.x) * VEC;
         if ((i + 1) * THREADS * VEC <= n)  // the whole block's
-            v[i] = load_whole<TYPE, NT>(p + e);
+            v[i] = load_run<TYPE, NT>(p + i * THREADS * VEC);
         else
-            v[i] = load_vec<TYPE, NT>(p, e, n, avail);
+            v[i] = load_vec<TYPE, NT>(p, (i * THREADS + threadIdx.x) * VEC, n, avail);
     }
 }
 
@@ -278,6 +300,10 @@ __device__ __forceinline__ uint32_t load_index(const void *p, uint64_t i, uint32
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// exp of a number that is not above 0: an argument x is off by 2^-24 x, which
+// takes at most 2e-8 of 1 from the result.
+__device__ __forceinline__ float exp_below(float x) { return exp2_fast(x * LOG2E); }
+
 // exp((x - m) / t) as 2^(x c - R) times 2^(R - m c), c = log2(e) / t and R the
 // whole number next to m c: one fused operation per number, whose only
 // rounding is that of a small result, and the second factor once.  R = 0 where
@@ -294,12 +320,12 @@ struct Base2 {
 };
 __device__ __forceinline__ bool sum_in_range(float s) { return s > 0.25f && s < 1e30f; }
 
-// ln of a sum: the exponent apart, so that the logarithm's own error stays
-// below 1e-7 however large the sum is
+// ln of a sum: the exponent apart, so that the logarithm's own error (of a
+// number in [0.5, 1)) stays below 1e-7 however large the sum is
 __device__ __forceinline__ double ln_sum(double x) {
     const int e = __builtin_amdgcn_frexp_exp(x);
     const float f = (float)__builtin_amdgcn_frexp_mant(x);
-    return (double)e * 0.6931471805599453 + (double)logf(f);
+    return 0.6931471805599453 * ((double)e + (double)__builtin_amdgcn_logf(f));
 }
 
 // A value of another lane of the row of 16 (DPP control word CTRL).
