@@ -313,8 +313,9 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
         if (at[i] < n) out[at[i]] = num_round<TYPE>(g[i]);
 }
 
-// A step of one row by one block.  The row's first RES vectors of every thread
-// stay in registers from the sum to the gradient.  What a longer row has beyond
+// A step (GRAD), or the forward pass of a row that THREADS threads hold, of one
+// row by one block.  A step's first RES vectors of every thread stay in
+// registers from the sum to the gradient.  What a longer row has beyond
 // them is read twice, MORE vectors at a time, the second time from the cache
 // beside the memory: 256 CUs hold at most 512 rows at a time, 128 MiB of 131072
 // 16-bit numbers, and it holds 256.  A CU's blocks are rarely in one phase, so
@@ -322,11 +323,12 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
 // largest kept logit, which is known before the row has arrived.
 constexpr int RES = 8;
 
-// Adds a run's numbers but for the kept columns, relative to a reference;
-// vector i THREADS + thread lies at bit (first + i THREADS + thread) VEC.
-template <uint32_t TYPE, uint32_t THREADS, int NV>
+// Adds a run's numbers but for the kept columns, relative to a reference, and
+// (MAX) takes their maximum; vector i THREADS + thread lies at bit (first +
+// i THREADS + thread) VEC.
+template <uint32_t TYPE, uint32_t THREADS, bool MAX, int NV>
 __device__ __forceinline__ float sum_run(Vec<TYPE> (&v)[NV], uint32_t n, uint32_t first, const uint32_t *bm,
-                                         const Base2 &to2, float sum) {
+                                         const Base2 &to2, float sum, uint32_t &bits) {
     constexpr uint32_t VEC = Num<TYPE>::VEC;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -334,6 +336,7 @@ __device__ __forceinline__ float sum_run(Vec<TYPE> (&v)[NV], uint32_t n, uint32_
         const uint32_t b = kept_bits<VEC>(bm, first + i * THREADS + threadIdx.x);
         if (b) v[i].mask(b);
         v[i].keep_packed();
+        if (MAX) bits = v[i].max_bits(bits);
 #pragma unroll
         for (uint32_t e = 0; e < VEC; ++e) sum += to2(v[i].get(e));
         asm volatile("" : "+v"(sum));  // one vector's numbers after the other
@@ -361,8 +364,8 @@ __device__ __forceinline__ void grad_run(Vec<TYPE> (&v)[NV], typename Num<TYPE>:
     }
 }
 
-template <uint32_t TYPE, uint32_t THREADS>
-__global__ __launch_bounds__(THREADS, THREADS < 512 ? 8 : 6) void k_distill_row(DistillArgs a) {
+template <uint32_t TYPE, uint32_t THREADS, bool GRAD>
+__global__ __launch_bounds__(THREADS, THREADS < 512 || !GRAD ? 8 : 6) void k_distill_row(DistillArgs a) {
     using N = Num<TYPE>;
     using T = typename N::T;
     constexpr uint32_t VEC = N::VEC, STEP = THREADS * VEC, CHUNK = RES * STEP;
@@ -379,8 +382,9 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 8 : 6) void k_distill_row(
     const float w = a.weight ? a.weight[row] : 1.f;
     if (w == 0.f) {
         const float zero[VEC] = {};
-        for (uint32_t e = threadIdx.x * VEC; e < n; e += STEP) store_vec<TYPE>(out, e, n, zero);
+        for (uint32_t e = threadIdx.x * VEC; GRAD && e < n; e += STEP) store_vec<TYPE>(out, e, n, zero);
         if (threadIdx.x == 0) a.loss[row] = 0.f;
+        if (!GRAD && a.stats && threadIdx.x < STATS) a.stats[row * STATS + threadIdx.x] = 0.f;
         return;
     }
     const T *p = (const T *)a.m.p + row * a.m.stride;
@@ -405,16 +409,21 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 8 : 6) void k_distill_row(
     lds_barrier();
     float ref = top > F_NEG_INF ? top : 0.f;
     const Base2 by_top(ref, a.c);
-    float sum = sum_run<TYPE, THREADS>(v, held, 0, bm, by_top, 0.f);
+    uint32_t bits = Vec<TYPE>::max_bits_none();
+    float sum = sum_run<TYPE, THREADS, !GRAD>(v, held, 0, bm, by_top, 0.f, bits);
 #pragma unroll 1
-    for (uint32_t e0 = CHUNK; e0 < n; e0 += MORE * STEP) {
+    for (uint32_t e0 = CHUNK; GRAD && e0 < n; e0 += MORE * STEP) {
         Vec<TYPE> u[MORE];
         load_slice<TYPE, THREADS, MORE, false>(u, p + e0, n - e0, avail - e0);
-        sum = sum_run<TYPE, THREADS>(u, n - e0, e0 / VEC, bm, by_top, sum);
+        sum = sum_run<TYPE, THREADS, false>(u, n - e0, e0 / VEC, bm, by_top, sum, bits);
     }
     sum = block_sum_f<THREADS>(sum, red[1]);
+    if (!GRAD) {  // the saved numbers are relative to the largest logit not kept
+        const float mx = block_max_f<THREADS>(Vec<TYPE>::max_value(bits), red[0]);
+        ref = mx > F_NEG_INF ? mx : ref;
+    }
     float tail = sum * by_top.to(ref);
-    if (!(sum > 1e-28f && sum < 1e30f)) {
+    if (!(sum > 1e-28f && sum < 1e30f && tail < 1e30f)) {
         const float2 x = slice_again<TYPE, THREADS>(p, n, avail, bm, a.c, red + 2);
         ref = x.x;
         tail = x.y;
@@ -429,12 +438,16 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 8 : 6) void k_distill_row(
         };
         const RowResult r = row_result(ref, tail, (a.t.k + 63) / 64, entry, a.t.rest ? a.t.rest[row] : F_NEG_INF, a.c,
                                        a.inv_t);
-        if (threadIdx.x == 0) {
-            a.loss[row] = (float)(w * r.loss);
+        if (threadIdx.x == 0) a.loss[row] = (float)(w * r.loss);
+        if (GRAD || a.stats) {
+            float st = 0.f;
 #pragma unroll
-            for (int i = 0; i < 6; ++i) row_stats[i] = r.stats[i];
+            for (uint32_t i = 0; i < 6; ++i) st = threadIdx.x == i ? r.stats[i] : st;
+            if (!GRAD && threadIdx.x < STATS) a.stats[row * STATS + threadIdx.x] = st;
+            if (GRAD && threadIdx.x < 6) row_stats[threadIdx.x] = st;
         }
     }
+    if constexpr (!GRAD) return;
     lds_barrier();
     const float m = row_stats[0] == F_NEG_INF ? 0.f : row_stats[0], scale = w * a.inv_t, q = scale * row_stats[1];
     ref = ref == F_NEG_INF ? 0.f : ref;
@@ -517,26 +530,39 @@ void grad_kernel(const DistillArgs &a, hipStream_t s) {
     trace_mark(s, "k_distill_grad");
 }
 
-// A step takes its rows one by one where they fill the chip and a row's bitmap
-// fits beside its entries.
+// Whether a step takes its rows one by one: where they are many, or so short
+// that a block is through with one as soon as it would be with a slice; and a
+// row's bitmap must fit beside its entries.  131072 bfloat16 columns, one by
+// one and by slices: 64 rows 18 and 14 us, 128 rows 20 and 21, 256 rows 29 and
+// 40; 32 rows of 32000: 9.6 and 10.5.
 constexpr uint32_t ROW_MAX_COLS = 1u << 18;
-bool rows_one_by_one(const Matrix &m) { return m.rows >= 512 && m.cols <= ROW_MAX_COLS; }
+bool step_by_rows(const Matrix &m) {
+    return m.cols <= ROW_MAX_COLS && (m.rows >= 128 || m.cols * type_bytes(m.type) <= 65536);
+}
+// A forward pass gains by rows of up to 256 threads' registers, being one
+// launch (4000 rows of 8000 bfloat16 columns: 20 us one by one, 24 by slices;
+// of 32000: 55 and 53).
+bool forward_by_rows(const Matrix &m) { return m.cols * type_bytes(m.type) <= 256 * RES * 16; }
 
-// Threads per row, as measured (us at 64, 128, 256, 512, 1024 threads, bfloat16):
-template <uint32_t TYPE>
+// Threads per row: as many as hold it in RES vectors each, but 512 up to twice
+// that, where three blocks share a CU and one of 1024 threads would have it for
+// itself (2048 x 65536 bfloat16: 100 us, and 122 with 1024).  At 256, 512 and
+// 1024 threads, 4096 x 131072 takes 494, 420 and 410 us; at 64, 128 and 256,
+// 30000 x 2000 takes 62, 85 and 110.
+template <uint32_t TYPE, bool GRAD>
 void row_kernel(const DistillArgs &a, hipStream_t s) {
     const uint32_t grid = (uint32_t)a.m.rows, vecs = (a.m.cols + Num<TYPE>::VEC - 1) / Num<TYPE>::VEC;
     const uint32_t lds = 4 * ((a.m.cols + 31) / 32 + 3 * a.t.k);
     if (vecs <= 64 * RES)
-        k_distill_row<TYPE, 64><<<grid, 64, lds, s>>>(a);
+        k_distill_row<TYPE, 64, GRAD><<<grid, 64, lds, s>>>(a);
     else if (vecs <= 128 * RES)
-        k_distill_row<TYPE, 128><<<grid, 128, lds, s>>>(a);
-    else if (vecs <= 256 * RES)
-        k_distill_row<TYPE, 256><<<grid, 256, lds, s>>>(a);
+        k_distill_row<TYPE, 128, GRAD><<<grid, 128, lds, s>>>(a);
+    else if (!GRAD || vecs <= 256 * RES)
+        k_distill_row<TYPE, 256, GRAD><<<grid, 256, lds, s>>>(a);
     else if (vecs <= 2 * 512 * RES)
-        k_distill_row<TYPE, 512><<<grid, 512, lds, s>>>(a);
+        k_distill_row<TYPE, 512, true><<<grid, 512, lds, s>>>(a);
     else
-        k_distill_row<TYPE, 1024><<<grid, 1024, lds, s>>>(a);
+        k_distill_row<TYPE, 1024, true><<<grid, 1024, lds, s>>>(a);
     trace_mark(s, "k_distill_row");
 }
 
@@ -567,6 +593,8 @@ hipError_t launch_distill_forward(const Matrix &m, const Teacher &t, float tempe
     a.part = (float2 *)ws;
     a.loss = loss_out;
     a.stats = stats_out;
+    if (forward_by_rows(m))
+        return by_type(m.type, [&](auto type) { row_kernel<decltype(type)::value, false>(a, s); });
     return by_type(m.type, [&](auto type) {
         slice_kernel<decltype(type)::value>(a, s);
         join_kernel<decltype(type)::value>(a, s);
@@ -587,12 +615,12 @@ hipError_t launch_distill_backward(const Matrix &m, const Teacher &t, float temp
 
 hipError_t launch_distill_step(const Matrix &m, const Teacher &t, float temperature, const float *weight,
                                float *loss_out, void *grad, uint64_t grad_stride, uint8_t *ws, hipStream_t s) {
-    if (rows_one_by_one(m)) {
+    if (step_by_rows(m)) {
         DistillArgs a = distill_args(m, t, temperature, weight);
         a.loss = loss_out;
         a.grad = grad;
         a.grad_stride = grad_stride;
-        return by_type(m.type, [&](auto type) { row_kernel<decltype(type)::value>(a, s); });
+        return by_type(m.type, [&](auto type) { row_kernel<decltype(type)::value, true>(a, s); });
     }
     float *stats = (float *)(ws + part_bytes(m));
     hipError_t e = launch_distill_forward(m, t, temperature, weight, loss_out, stats, ws, s);
