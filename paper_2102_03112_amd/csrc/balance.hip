@@ -157,10 +157,7 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
         }
     }
 #pragma unroll
-    for (uint32_t i = 0; i < N; ++i) {  // the wave's rows
-#pragma unroll
-        for (uint32_t o = LANES; o < 64; o <<= 1) acc[i] += __shfl_xor(acc[i], o, 64);
-    }
+    for (uint32_t i = 0; i < N; ++i) acc[i] = groups_sum<LANES>(acc[i]);  // the wave's rows
     if (lane < LANES) {
 #pragma unroll
         for (uint32_t i = 0; i < N; ++i) sums[w][(i / VEC * LANES + sub) * VEC + i % VEC] = acc[i];
@@ -206,9 +203,14 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
 
 // Groups of several blocks: joined JOIN_COLS columns a block, so that the
 // partial sums of a large batch (1024 blocks x 256 experts: 2 MiB) are read by
-// many; every block counts the group's rows for itself.
-constexpr uint32_t JT = 512, JOIN_COLS = 16, JOIN_WAYS = JT / JOIN_COLS;
+// many; every block counts the group's rows for itself.  One group of up to 256
+// blocks and ONE_JOIN_COLS experts is joined by a single block, which has the
+// loss, too (16384 x 64: 9.9 us in all, and 10.6 with two launches more; of
+// 1024 blocks 17.2 and 14.9).
+constexpr uint32_t JOIN_COLS = 16, ONE_JOIN_COLS = 64;
+template <uint32_t JT, uint32_t JOIN_COLS>
 __global__ __launch_bounds__(JT) void k_balance_join(BalanceArgs a) {
+    constexpr uint32_t JOIN_WAYS = JT / JOIN_COLS;
     __shared__ double sums[JOIN_WAYS][JOIN_COLS];
     __shared__ uint32_t counts[JOIN_WAYS][JOIN_COLS];
     __shared__ uint32_t rows;
@@ -307,7 +309,7 @@ __global__ __launch_bounds__(BT) void k_balance_grad(BalanceArgs a) {
     }
 }
 
-constexpr uint32_t MAX_PARTS = 2048;
+constexpr uint32_t MAX_PARTS = 1024;
 
 // How a type's rows lie over lanes, and the blocks that a call takes.
 struct Shape {
@@ -321,7 +323,7 @@ Shape plan_rows(uint64_t rows, uint32_t experts, uint32_t type, uint32_t group_r
     s.ni = (vecs + 63) / 64;
     const uint64_t groups = rows ? (rows + group_rows - 1) / group_rows : 0;
     const uint64_t own = std::min<uint64_t>(rows, group_rows), step = BW * (64 / s.lanes);
-    // eight blocks per CU in all, but two rounds of a block's waves at least
+    // four blocks per CU in all, but two rounds of a block's waves at least
     uint64_t parts = std::max<uint64_t>(1, MAX_PARTS / std::max<uint64_t>(1, groups));
     parts = std::max<uint64_t>(1, std::min(parts, own / (2 * step)));
     const uint64_t per = own ? (own + parts - 1) / parts : 1;
@@ -394,7 +396,8 @@ hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, 
     BalanceArgs a = balance_args(m, r, coef, sh);
     const uint64_t blocks = (uint64_t)r.groups * sh.parts;
     a.gloss = (double *)ws;
-    a.col_blocks = (m.cols + JOIN_COLS - 1) / JOIN_COLS;
+    const bool one = r.groups == 1 && m.cols <= ONE_JOIN_COLS && sh.parts <= 256;
+    a.col_blocks = one ? 1 : (m.cols + JOIN_COLS - 1) / JOIN_COLS;
     a.partial = (uint2 *)(a.gloss + (sh.parts > 1 ? r.groups * a.col_blocks : r.groups));
     a.prows = (uint32_t *)(a.partial + blocks * m.cols);
     a.counts_out = counts_out;
@@ -408,7 +411,10 @@ hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, 
     uint32_t losses = r.groups;
     if (sh.parts > 1) {
         losses *= a.col_blocks;
-        k_balance_join<<<losses, JT, 0, s>>>(a);
+        if (one)
+            k_balance_join<1024, ONE_JOIN_COLS><<<1, 1024, 0, s>>>(a);
+        else
+            k_balance_join<512, JOIN_COLS><<<losses, 512, 0, s>>>(a);
         trace_mark(s, "k_balance_join");
     }
     if (losses != 1) {

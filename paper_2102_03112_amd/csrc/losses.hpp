@@ -362,6 +362,24 @@ template <uint32_t LANES>
 __device__ __forceinline__ float lanes_sum(float v) {
     return lanes_reduce<LANES>(v, [](float a, float b) { return a + b; });
 }
+// Sum over the lanes of one place in every aligned group of LANES lanes: by
+// rotations of the rows of 16, which keep a place, then over rows and halves.
+template <uint32_t LANES>
+__device__ __forceinline__ float groups_sum(float v) {
+    if constexpr (LANES <= 8) v += dpp<0x128>(v);
+    if constexpr (LANES <= 4) v += dpp<0x124>(v);
+    if constexpr (LANES <= 2) v += dpp<0x122>(v);
+    if constexpr (LANES <= 1) v += dpp<0x121>(v);
+    if constexpr (LANES <= 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if constexpr (LANES <= 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return v;
+}
 __device__ __forceinline__ float wave_max_f(float v) { return lanes_max<64>(v); }
 __device__ __forceinline__ float wave_sum_f(float v) { return lanes_sum<64>(v); }
 
