@@ -414,26 +414,29 @@ __device__ __forceinline__ float block_sum_f(float v, float *scratch) {
 struct Slices {
     uint32_t nv, len, n;
 };
-// The longest slices (fewest results to join) that give `blocks` blocks; 512
-// are two for each of the 256 CUs.
+// The longest slices (fewest results to join) that give `blocks` blocks, 512
+// being two for each of the 256 CUs, and as few vectors as such a slice needs.
 inline Slices plan_slices(uint64_t rows, uint64_t cols, uint32_t vec, uint32_t threads, uint32_t nv_max,
                           uint64_t blocks = 512) {
     Slices s;
+    uint64_t cap, n;
     for (s.nv = nv_max;; s.nv /= 2) {
-        const uint64_t cap = (uint64_t)threads * s.nv * vec;
-        const uint64_t n = (cols + cap - 1) / cap;
-        if (rows * n < blocks && s.nv > 1) continue;
-        const uint64_t len = (cols + n - 1) / n;
-        s.len = (uint32_t)std::min<uint64_t>(cap, (len + vec - 1) / vec * vec);
-        s.n = (uint32_t)((cols + s.len - 1) / s.len);
-        return s;
+        cap = (uint64_t)threads * s.nv * vec;
+        n = (cols + cap - 1) / cap;
+        if (rows * n >= blocks || s.nv == 1) break;
     }
+    const uint64_t len = (cols + n - 1) / n;
+    s.len = (uint32_t)std::min<uint64_t>(cap, (len + vec - 1) / vec * vec);
+    s.n = (uint32_t)((cols + s.len - 1) / s.len);
+    while (s.nv > 1 && (uint64_t)threads * (s.nv / 2) * vec >= s.len) s.nv /= 2;
+    return s;
 }
 
 // toplogits.hip
-constexpr uint32_t TOP_THREADS = 512, TOP_NV = 8;
+constexpr uint32_t TOP_NV = 8;
 constexpr uint32_t TOP_JOIN = 2048;  // list entries that one block joins
 struct TopPlan {
+    uint32_t threads;    // of a slice's block
     Slices sl;
     uint32_t fan;        // lists that one block joins
     uint64_t lists[2];   // most lists that the two buffers hold per row

@@ -20,9 +20,10 @@
 namespace dr {
 namespace {
 
-constexpr uint32_t NT = TOP_THREADS, NW = NT / 64;
-constexpr uint32_t CAND = 1024;  // listed logits per slice: four times the largest K
-// room for what one wave lists: all that it holds, or eight times an even share of the largest K
+// A slice's block of NT threads takes K up to NT / 2, and has room to list four
+// times that; one wave may list all that it holds, or eight times an even share.
+template <uint32_t NT>
+constexpr uint32_t CAND = 2 * NT;
 template <int NV>
 constexpr uint32_t WAVE_CAND = NV == 1 ? 512 : 256;
 
@@ -66,9 +67,11 @@ __device__ __forceinline__ uint32_t wave_nth16(uint32_t key, uint32_t n) {
     return t;
 }
 
+template <uint32_t NT>
 struct TopShared {
-    uint64_t cand[CAND], sorted[CAND];
-    uint32_t rank[CAND];
+    static constexpr uint32_t NW = NT / 64;
+    uint64_t cand[CAND<NT>], sorted[CAND<NT>];
+    uint32_t rank[CAND<NT>];
     uint32_t count;
     uint32_t bound[NW], reached[NW], listed[NW];
     uint32_t scan[NW + 1];
@@ -143,7 +146,7 @@ __device__ __forceinline__ void top_finish(const TopArgs &a, uint64_t row, uint6
 
 // A slice as the rare paths read it: again from memory, one vector per thread
 // and step, so that they cost the usual path no registers.
-template <uint32_t TYPE>
+template <uint32_t TYPE, uint32_t NT>
 struct SliceView {
     const typename Num<TYPE>::T *p;
     uint64_t avail;
@@ -158,12 +161,13 @@ struct SliceView {
     }
 };
 
-// For a slice with more than CAND logits above -inf: lists exactly K, those
+// For a slice with more than K logits above -inf: lists exactly K, those
 // above the K-th largest, found bit by bit, and of those equal to it the ones
 // of lowest column.  Returns the K-th largest; *equal receives how many are
 // equal to it and not listed.
-template <uint32_t TYPE>
-__device__ __forceinline__ float top_exact(const SliceView<TYPE> &sl, uint32_t K, TopShared &sh, uint32_t *equal) {
+template <uint32_t TYPE, uint32_t NT>
+__device__ __forceinline__ float top_exact(const SliceView<TYPE, NT> &sl, uint32_t K, TopShared<NT> &sh,
+                                           uint32_t *equal) {
     constexpr uint32_t VEC = Num<TYPE>::VEC;
     if (threadIdx.x < 32) sh.bits[threadIdx.x] = 0;
     if (threadIdx.x == 0) sh.count = 0;
@@ -226,8 +230,9 @@ __device__ __forceinline__ float top_exact(const SliceView<TYPE> &sl, uint32_t K
 
 // (reference, sum) of a slice's logits below the bound, relative to their own
 // largest; red: two sets of scratch.
-template <uint32_t TYPE>
-__device__ __forceinline__ float2 sum_below(const SliceView<TYPE> &sl, float bound, float c, float (*red)[NW]) {
+template <uint32_t TYPE, uint32_t NT>
+__device__ __forceinline__ float2 sum_below(const SliceView<TYPE, NT> &sl, float bound, float c,
+                                            float (*red)[NT / 64]) {
     constexpr uint32_t VEC = Num<TYPE>::VEC;
     float mx = F_NEG_INF;
 #pragma unroll 1
@@ -248,17 +253,17 @@ __device__ __forceinline__ float2 sum_below(const SliceView<TYPE> &sl, float bou
     return make_float2(mx, block_sum_f<NT>(sum, red[1]));
 }
 
-template <uint32_t TYPE, int NV>
+template <uint32_t TYPE, int NV, uint32_t NT>
 __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
     using N = Num<TYPE>;
-    constexpr uint32_t VEC = N::VEC;
-    __shared__ TopShared sh;
+    constexpr uint32_t VEC = N::VEC, NW = NT / 64;
+    __shared__ TopShared<NT> sh;
     __shared__ uint2 wave_cand[NW][WAVE_CAND<NV>];  // a listed logit and its column in the slice
     const uint64_t row = blockIdx.x / a.sl.n;
     const uint32_t s = blockIdx.x % a.sl.n, start = s * a.sl.len, n = min(a.sl.len, a.m.cols - start);
     const auto *p = (const typename N::T *)a.m.p + row * a.m.stride + start;
     const uint64_t avail = row_avail(a.m, row) - start;
-    const SliceView<TYPE> sl = {p, avail, start, n};
+    const SliceView<TYPE, NT> sl = {p, avail, start, n};
     Vec<TYPE> v[NV];
     load_slice<TYPE, NT>(v, p, n, avail);
     if (threadIdx.x < NW) sh.reached[threadIdx.x] = 0;
@@ -319,18 +324,18 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
         count += sh.listed[i];
         exact |= sh.listed[i] > WAVE_CAND<NV>;
     }
-    exact |= count > CAND;
+    exact |= count > CAND<NT>;
     if (!exact)
         for (uint32_t i = threadIdx.x & 63u; i < listed; i += 64)
             sh.cand[before + i] = top_key(__uint_as_float(wave_cand[w][i].x), start + wave_cand[w][i].y);
     sum = block_sum_f<NT>(sum, sh.red[0]) * to2.to(bound);
     if (exact) {
-        bound = top_exact<TYPE>(sl, a.k, sh, &equal);
+        bound = top_exact<TYPE, NT>(sl, a.k, sh, &equal);
         count = sh.count;
     }
     // other logits than these are listed, or all that was added lies far below the bound
     if (exact || !(sum > 1e-20f && sum < 1e30f)) {
-        const float2 x = sum_below<TYPE>(sl, bound, a.c, sh.red + 1);
+        const float2 x = sum_below<TYPE, NT>(sl, bound, a.c, sh.red + 1);
         ref = x.x;
         sum = x.y;
         if (equal) {
@@ -405,16 +410,26 @@ __global__ __launch_bounds__(JT) void k_top_join(TopArgs a) {
 }
 constexpr uint32_t FEW_ENTRIES = 512;
 
-template <uint32_t TYPE>
+template <uint32_t TYPE, uint32_t NT>
 void slice_kernel(const TopArgs &a, hipStream_t s) {
     const uint32_t grid = (uint32_t)(a.m.rows * a.sl.n);
     switch (a.sl.nv) {
-        case 1: k_top_slice<TYPE, 1><<<grid, NT, 0, s>>>(a); break;
-        case 2: k_top_slice<TYPE, 2><<<grid, NT, 0, s>>>(a); break;
-        case 4: k_top_slice<TYPE, 4><<<grid, NT, 0, s>>>(a); break;
-        default: k_top_slice<TYPE, 8><<<grid, NT, 0, s>>>(a); break;
+        case 1: k_top_slice<TYPE, 1, NT><<<grid, NT, 0, s>>>(a); break;
+        case 2: k_top_slice<TYPE, 2, NT><<<grid, NT, 0, s>>>(a); break;
+        case 4: k_top_slice<TYPE, 4, NT><<<grid, NT, 0, s>>>(a); break;
+        default: k_top_slice<TYPE, 8, NT><<<grid, NT, 0, s>>>(a); break;
     }
     trace_mark(s, "k_top_slice");
+}
+
+template <uint32_t TYPE>
+void slice_kernel(const TopArgs &a, uint32_t threads, hipStream_t s) {
+    if (threads == 128)
+        slice_kernel<TYPE, 128>(a, s);
+    else if (threads == 256)
+        slice_kernel<TYPE, 256>(a, s);
+    else
+        slice_kernel<TYPE, 512>(a, s);
 }
 
 uint64_t list_bytes(uint64_t rows, uint64_t lists, uint32_t k) {
@@ -425,7 +440,13 @@ uint64_t list_bytes(uint64_t rows, uint64_t lists, uint32_t k) {
 
 TopPlan plan_top(uint64_t rows, uint64_t cols, uint32_t k, uint32_t type) {
     TopPlan p = {};
-    p.sl = plan_slices(rows, cols, 16 / type_bytes(type), TOP_THREADS, TOP_NV);
+    // the fewest threads that hold a row and are twice K, if rows fill the chip; else a slice costs a block much the
+    // same whatever its length, so slices are long
+    const uint32_t vec = 16 / type_bytes(type);
+    p.threads = 512;
+    for (uint32_t t = 128; t < 512; t *= 2)
+        if (p.threads == 512 && rows >= 512 && 2 * k <= t && cols <= (uint64_t)t * TOP_NV * vec) p.threads = t;
+    p.sl = plan_slices(rows, cols, vec, p.threads, TOP_NV);
     p.fan = std::max(2u, TOP_JOIN / k);
     p.lists[0] = p.sl.n > 1 ? p.sl.n : 0;
     p.lists[1] = p.sl.n > p.fan ? (p.sl.n + p.fan - 1) / p.fan : 0;
@@ -455,9 +476,9 @@ hipError_t launch_top(const Matrix &m, uint32_t k, float temperature, int32_t *i
         a.sums = sums[0];
     }
     switch (m.type) {
-        case TYPE_F32: slice_kernel<TYPE_F32>(a, s); break;
-        case TYPE_BF16: slice_kernel<TYPE_BF16>(a, s); break;
-        default: slice_kernel<TYPE_F16>(a, s); break;
+        case TYPE_F32: slice_kernel<TYPE_F32>(a, p.threads, s); break;
+        case TYPE_BF16: slice_kernel<TYPE_BF16>(a, p.threads, s); break;
+        default: slice_kernel<TYPE_F16>(a, p.threads, s); break;
     }
     uint32_t lists = p.sl.n;
     for (int from = 0; lists > 1; from ^= 1) {
