@@ -416,7 +416,9 @@ void slice_kernel(const TopArgs &a, hipStream_t s) {
     switch (a.sl.nv) {
         case 1: k_top_slice<TYPE, 1, NT><<<grid, NT, 0, s>>>(a); break;
         case 2: k_top_slice<TYPE, 2, NT><<<grid, NT, 0, s>>>(a); break;
+        case 3: k_top_slice<TYPE, 3, NT><<<grid, NT, 0, s>>>(a); break;
         case 4: k_top_slice<TYPE, 4, NT><<<grid, NT, 0, s>>>(a); break;
+        case 6: k_top_slice<TYPE, 6, NT><<<grid, NT, 0, s>>>(a); break;
         default: k_top_slice<TYPE, 8, NT><<<grid, NT, 0, s>>>(a); break;
     }
     trace_mark(s, "k_top_slice");
@@ -447,6 +449,9 @@ TopPlan plan_top(uint64_t rows, uint64_t cols, uint32_t k, uint32_t type) {
     for (uint32_t t = 128; t < 512; t *= 2)
         if (p.threads == 512 && rows >= 512 && 2 * k <= t && cols <= (uint64_t)t * TOP_NV * vec) p.threads = t;
     p.sl = plan_slices(rows, cols, vec, p.threads, TOP_NV);
+    // vectors that the slices need, of 1, 2, 3, 4, 6 and 8
+    const uint32_t nv = (p.sl.len + p.threads * vec - 1) / (p.threads * vec);
+    p.sl.nv = nv == 5 ? 6 : nv == 7 ? 8 : nv;
     p.fan = std::max(2u, TOP_JOIN / k);
     p.lists[0] = p.sl.n > 1 ? p.sl.n : 0;
     p.lists[1] = p.sl.n > p.fan ? (p.sl.n + p.fan - 1) / p.fan : 0;
