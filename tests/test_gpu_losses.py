@@ -40,6 +40,8 @@ TOP_SHAPES = [
     (1, 1, 1), (2, 1, 3), (3, 2, 1), (3, 7, 5), (2, 9, 9), (1, 63, 10), (2, 65, 64), (5, 257, 16), (3, 1000, 256),
     (2, 4095, 50), (2, 4096, 50), (2, 4097, 50), (1, 8193, 1), (2, 16385, 100), (1, 33000, 256), (3, 50001, 64),
     (600, 700, 20), (530, 5001, 33), (1, 131073, 64), (1, 300007, 256),
+    # rows enough for small blocks
+    (512, 3000, 60), (513, 9001, 64), (515, 9001, 65), (512, 13000, 128), (520, 14001, 200),
 ]
 
 
@@ -191,6 +193,8 @@ DISTILL_SHAPES = [
     (1, 1, 1), (2, 2, 1), (3, 5, 5), (4, 9, 3), (2, 64, 8), (3, 255, 255), (2, 1000, 64), (3, 2047, 100),
     (3, 2048, 100), (3, 2049, 100), (2, 16384, 50), (2, 16385, 50), (5, 20011, 256), (300, 300, 20), (260, 2100, 7),
     (2, 40000, 1000), (1, 131072, 64), (2, 140001, 32),
+    # rows enough for a block each, of lengths that take other blocks, one and several rounds of them
+    (130, 520, 9), (128, 4097, 30), (131, 8200, 16), (128, 16400, 300), (129, 33000, 12), (128, 70003, 40),
 ]
 
 
