@@ -19,6 +19,9 @@
  * capture would refuse.  Results do not depend on the order in which blocks
  * run: the same inputs give the same bits.
  *
+ * A launch counts its threads in 32 bits: rows x cols that would need more
+ * (some 10^11 numbers, or 10^7 groups of a balance loss) are EINVAL.
+ *
  * Logits.  A matrix of rows x cols numbers of one type, each row contiguous,
  * rows `row_stride` numbers apart; any alignment that suits the type.  -inf
  * masks a column.  +inf and NaN are outside the contract: the outputs of that

@@ -390,6 +390,12 @@ size_t balance_ws_bytes(uint64_t rows, uint64_t experts) {
     return 8 * std::max<uint64_t>(rows, joining) + MAX_PARTS * (8 * experts + 4);
 }
 
+uint64_t balance_threads(const Matrix &m, const Routes &r) {
+    const uint64_t joining = (uint64_t)r.groups * ((m.cols + JOIN_COLS - 1) / JOIN_COLS) * 512;
+    const Shape sh = plan_rows(m.rows, m.cols, m.type, r.group_rows);
+    return std::max((uint64_t)r.groups * sh.parts * BT, sh.parts > 1 ? joining : 0);
+}
+
 hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, int32_t *counts_out,
                                   int32_t *rows_out, float *prob_out, float *loss_out, uint8_t *ws, hipStream_t s) {
     const Shape sh = plan_rows(m.rows, m.cols, m.type, r.group_rows);

@@ -549,17 +549,23 @@ bool forward_by_rows(const Matrix &m) { return m.cols * type_bytes(m.type) <= 25
 // itself (2048 x 65536 bfloat16: 100 us, and 122 with 1024).  At 256, 512 and
 // 1024 threads, 4096 x 131072 takes 494, 420 and 410 us; at 64, 128 and 256,
 // 30000 x 2000 takes 62, 85 and 110.
+uint32_t row_threads(const Matrix &m) {
+    const uint32_t vec = 16 / type_bytes(m.type), vecs = (m.cols + vec - 1) / vec;
+    for (uint32_t t = 64; t <= 256; t *= 2)
+        if (vecs <= t * RES) return t;
+    return vecs <= 2 * 512 * RES ? 512 : 1024;
+}
 template <uint32_t TYPE, bool GRAD>
 void row_kernel(const DistillArgs &a, hipStream_t s) {
-    const uint32_t grid = (uint32_t)a.m.rows, vecs = (a.m.cols + Num<TYPE>::VEC - 1) / Num<TYPE>::VEC;
+    const uint32_t grid = (uint32_t)a.m.rows, threads = row_threads(a.m);
     const uint32_t lds = 4 * ((a.m.cols + 31) / 32 + 3 * a.t.k);
-    if (vecs <= 64 * RES)
+    if (threads == 64)
         k_distill_row<TYPE, 64, GRAD><<<grid, 64, lds, s>>>(a);
-    else if (vecs <= 128 * RES)
+    else if (threads == 128)
         k_distill_row<TYPE, 128, GRAD><<<grid, 128, lds, s>>>(a);
-    else if (!GRAD || vecs <= 256 * RES)
+    else if (!GRAD || threads == 256)
         k_distill_row<TYPE, 256, GRAD><<<grid, 256, lds, s>>>(a);
-    else if (vecs <= 2 * 512 * RES)
+    else if (threads == 512)
         k_distill_row<TYPE, 512, true><<<grid, 512, lds, s>>>(a);
     else
         k_distill_row<TYPE, 1024, true><<<grid, 1024, lds, s>>>(a);
@@ -581,6 +587,10 @@ hipError_t by_type(uint32_t type, F f) {
 size_t part_bytes(const Matrix &m) { return (m.rows * distill_slices(m).n * sizeof(float2) + 255) / 256 * 256; }
 
 }  // namespace
+
+uint64_t distill_threads(const Matrix &m) {
+    return m.rows * std::max<uint64_t>(row_threads(m), (uint64_t)distill_slices(m).n * DIST_THREADS);
+}
 
 size_t distill_ws_bytes(uint64_t rows, uint64_t cols, uint32_t type) {
     const Matrix m = {nullptr, rows, cols, (uint32_t)cols, type};

@@ -432,6 +432,9 @@ inline Slices plan_slices(uint64_t rows, uint64_t cols, uint32_t vec, uint32_t t
     return s;
 }
 
+// A launch's threads are counted in 32 bits.
+constexpr uint64_t MAX_THREADS = 0xffffffffull;
+
 // toplogits.hip
 constexpr uint32_t TOP_NV = 8;
 constexpr uint32_t TOP_JOIN = 2048;  // list entries that one block joins
@@ -455,6 +458,7 @@ struct Teacher {
 };
 constexpr uint32_t DIST_THREADS = 256, DIST_NV = 8;
 size_t distill_ws_bytes(uint64_t rows, uint64_t cols, uint32_t type);
+uint64_t distill_threads(const Matrix &m);  // of the largest launch
 hipError_t launch_distill_forward(const Matrix &m, const Teacher &t, float temperature, const float *weight,
                                   float *loss_out, float *stats_out, uint8_t *ws, hipStream_t s);
 hipError_t launch_distill_backward(const Matrix &m, const Teacher &t, float temperature, const float *weight,
@@ -472,6 +476,7 @@ struct Routes {
     uint32_t group_rows, groups;
 };
 size_t balance_ws_bytes(uint64_t rows, uint64_t experts);
+uint64_t balance_threads(const Matrix &m, const Routes &r);  // of the largest launch
 hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, int32_t *counts_out,
                                   int32_t *rows_out, float *prob_out, float *loss_out, uint8_t *ws, hipStream_t s);
 hipError_t launch_balance_backward(const Matrix &m, const Routes &r, float coef, const int32_t *counts,

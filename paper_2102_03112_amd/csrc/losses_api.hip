@@ -78,8 +78,7 @@ dr_status check_distill(const dr_logits *student_h, const dr_teacher *teacher_h,
     if (st == DR_OK) st = check_teacher(teacher_h, m, t);
     if (st == DR_OK) st = check_temperature(temperature);
     if (st != DR_OK) return st;
-    if (m.rows * plan_slices(m.rows, m.cols, 16 / type_bytes(m.type), DIST_THREADS, DIST_NV).n >= MAX_ROWS)
-        return fail(DR_EINVAL, "rows times cols too large for one call");
+    if (distill_threads(m) > MAX_THREADS) return fail(DR_EINVAL, "rows times cols too large for one call");
     return DR_OK;
 }
 
@@ -100,6 +99,7 @@ dr_status check_routes(const dr_logits *router_h, const dr_routes *r, float coef
     }
     out = {r->idx, r->row_mask, r->idx_stride, r->k, r->idx_type, (uint32_t)r->group_rows,
            (uint32_t)ceil_div(m.rows, r->group_rows)};
+    if (balance_threads(m, out) > MAX_THREADS) return fail(DR_EINVAL, "too many groups for one call");
     return DR_OK;
 }
 
@@ -134,7 +134,8 @@ dr_status dr_top_logits(const dr_logits *logits_h, uint32_t k, float temperature
     if (k < 1 || k > DR_MAX_TOP) return fail(DR_EINVAL, "k must be in 1 .. %u", DR_MAX_TOP);
     if ((!idx_out || !val_out) && m.rows > 0) return fail(DR_EINVAL, "null output pointer");
     const TopPlan p = plan_top(m.rows, m.cols, k, m.type);
-    if (m.rows * p.sl.n >= MAX_ROWS) return fail(DR_EINVAL, "rows times cols too large for one call");
+    // the joins' blocks are no larger than the slices', and fewer
+    if (m.rows * p.sl.n * p.threads > MAX_THREADS) return fail(DR_EINVAL, "rows times cols too large for one call");
     if (p.bytes && !ws_ok(ws, ws_bytes, p.bytes)) return ws_small(p.bytes);
     if (m.rows == 0) return DR_OK;
     const hipStream_t s = (hipStream_t)stream;

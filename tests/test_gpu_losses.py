@@ -619,3 +619,26 @@ def test_results_do_not_hang_on_the_workspace():
     for other in seen[1:]:
         for a, b in zip(seen[0], other):
             assert torch.equal(a, b)
+
+
+def test_matrices_of_more_than_2_to_the_32_numbers():
+    """The last rows of a matrix whose offsets pass 32 bits, against the same rows by themselves: the same kernels, so
+    the same bits."""
+    rows, cols, k, few = 33_000, 131_072, 8, 200
+    gen = torch.Generator(device="cuda").manual_seed(109)
+    z = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    assert rows * cols > 1 << 32
+    z[-few:] = 3.0 * torch.randn(few, cols, generator=gen, device="cuda")
+    z[:few] = torch.randn(few, cols, generator=gen, device="cuda")
+    last = z[-few:].clone()
+    big, small = run_top(z, k), run_top(last, k)
+    for a, b in zip(big, small):
+        assert torch.equal(a[-few:], b)
+    weight = torch.zeros(rows, device="cuda")
+    weight[-few:] = 1.0
+    loss, part = torch.full((rows,), 7.0, device="cuda"), torch.full((few,), 7.0, device="cuda")
+    grad = torch.zeros_like(last)
+    L.distill_step(last, L.Teacher(*small), 1.0, None, part, grad, L.workspace(few, cols, k))
+    L.distill_step(z, L.Teacher(*big), 1.0, weight, loss, z, L.workspace(rows, cols, k))
+    assert torch.equal(loss[-few:], part) and torch.equal(z[-few:], grad)
+    assert float(loss[:-few].abs().max()) == 0.0 and float(z[:few].abs().max()) == 0.0

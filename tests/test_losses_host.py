@@ -143,6 +143,8 @@ def test_missing_and_bad_outputs_are_refused(lib):
 def test_calls_too_large_for_one_grid_are_refused(lib):
     lg = logits(rows=1 << 20, cols=1 << 28, row_stride=1 << 28)
     refused(lib, ("top",) + DISTILL, lg, gs=1 << 28)
+    refused(lib, ("top",) + DISTILL, logits(rows=1 << 30, cols=8, row_stride=8), gs=8)
+    refused(lib, BALANCE, logits(rows=1 << 28), ro=routes(group_rows=1))
 
 
 def test_small_workspaces_are_refused(lib):
