@@ -480,7 +480,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 || !GRAD ? 8 : 6) void k_dis
 }
 
 Slices distill_slices(const Matrix &m) {
-    return plan_slices(m.rows, m.cols, 16 / type_bytes(m.type), DIST_THREADS, DIST_NV);
+    return plan_slices(m.rows, m.cols, 16 / type_bytes(m.type), DIST_THREADS, DIST_NV, 512);
 }
 
 DistillArgs distill_args(const Matrix &m, const Teacher &t, float temperature, const float *weight) {

@@ -414,10 +414,10 @@ __device__ __forceinline__ float block_sum_f(float v, float *scratch) {
 struct Slices {
     uint32_t nv, len, n;
 };
-// The longest slices (fewest results to join) that give `blocks` blocks, 512
-// being two for each of the 256 CUs, and as few vectors as such a slice needs.
+// The longest slices (fewest results to join) that give `blocks` blocks, and as
+// few vectors as such a slice needs.
 inline Slices plan_slices(uint64_t rows, uint64_t cols, uint32_t vec, uint32_t threads, uint32_t nv_max,
-                          uint64_t blocks = 512) {
+                          uint64_t blocks) {
     Slices s;
     uint64_t cap, n;
     for (s.nv = nv_max;; s.nv /= 2) {
