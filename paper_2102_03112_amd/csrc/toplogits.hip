@@ -67,10 +67,27 @@ __device__ __forceinline__ uint32_t wave_nth16(uint32_t key, uint32_t n) {
     return t;
 }
 
+// The largest of the NW (up to 8) numbers that lane i % NW has of i, on every lane.
+template <uint32_t NW>
+__device__ __forceinline__ uint32_t lanes_max_u(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp(v, DPP_XOR1, 0xf, 0xf, true));
+    if constexpr (NW >= 4) v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp(v, DPP_XOR2, 0xf, 0xf, true));
+    if constexpr (NW >= 8) v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp(v, DPP_MIRROR8, 0xf, 0xf, true));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+// The sum of lanes 0 .. i on lane i < 8.
+__device__ __forceinline__ uint32_t first_lanes_scan(uint32_t v) {
+    v += __builtin_amdgcn_mov_dpp(v, 0x111, 0xf, 0xf, true);  // shifts by 1, 2 and 4, 0 moving in
+    v += __builtin_amdgcn_mov_dpp(v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_mov_dpp(v, 0x114, 0xf, 0xf, true);
+    return v;
+}
+
 template <uint32_t NT>
 struct TopShared {
     static constexpr uint32_t NW = NT / 64;
-    uint64_t cand[CAND<NT>], sorted[CAND<NT>];
+    alignas(16) uint64_t cand[CAND<NT>];
+    uint64_t sorted[CAND<NT>];
     uint32_t rank[CAND<NT>];
     uint32_t count;
     uint32_t bound[NW], reached[NW], listed[NW];
@@ -84,28 +101,38 @@ __device__ __forceinline__ float top_rescale(float x, float a, float b, float c)
     return x == 0.f ? 0.f : x * exp2_fast((a - b) * c);
 }
 
+// How many of keys[0 .. n) are above `key`; n is a multiple of RANK_STEP.
+constexpr uint32_t RANK_STEP = 4;
+__device__ __forceinline__ uint32_t keys_above(const uint64_t *keys, uint32_t n, uint64_t key) {
+    uint32_t r = 0;
+#pragma unroll 1
+    for (uint32_t j = 0; j < n; j += RANK_STEP) {
+        const ulonglong2 a = *(const ulonglong2 *)(keys + j), b = *(const ulonglong2 *)(keys + j + 2);
+        r += a.x > key ? 1u : 0u;
+        r += a.y > key ? 1u : 0u;
+        r += b.x > key ? 1u : 0u;
+        r += b.y > key ? 1u : 0u;
+    }
+    return r;
+}
+
 // sorted[] := the n keys of in[] in descending order, by counting the keys
-// before each, which the block's threads share where keys are few.
+// before each, which the block's threads share where keys are few: as many
+// threads as the keys (in whole waves) count in one run of them each, and the
+// last run is filled up with 0, which is no key and above none.  in[] has room
+// for that, being a multiple of RANK_STEP and twice the threads.
 template <uint32_t THREADS>
-__device__ __forceinline__ void rank_keys(const uint64_t *in, uint32_t n, uint32_t *rank, uint64_t *sorted) {
+__device__ __forceinline__ void rank_keys(uint64_t *in, uint32_t n, uint32_t *rank, uint64_t *sorted) {
     const uint32_t lanes = (n + 63u) & ~63u, ways = lanes && lanes < THREADS ? THREADS / lanes : 1u;
+    const uint32_t run = ((n + ways - 1) / ways + RANK_STEP - 1) / RANK_STEP * RANK_STEP;
     for (uint32_t i = threadIdx.x; i < n; i += THREADS) rank[i] = 0;
+    if (n + threadIdx.x < ways * run) in[n + threadIdx.x] = 0;
     __syncthreads();
     if (ways > 1) {
         const uint32_t way = threadIdx.x / lanes, i = threadIdx.x % lanes;
-        if (way < ways && i < n) {
-            const uint64_t key = in[i];
-            uint32_t r = 0;
-            for (uint32_t j = way; j < n; j += ways) r += in[j] > key ? 1u : 0u;
-            atomicAdd(&rank[i], r);
-        }
+        if (way < ways && i < n) atomicAdd(&rank[i], keys_above(in + way * run, run, in[i]));
     } else {
-        for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
-            const uint64_t key = in[i];
-            uint32_t r = 0;
-            for (uint32_t j = 0; j < n; ++j) r += in[j] > key ? 1u : 0u;
-            rank[i] = r;
-        }
+        for (uint32_t i = threadIdx.x; i < n; i += THREADS) rank[i] = keys_above(in, run, in[i]);
     }
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < n; i += THREADS) sorted[rank[i]] = in[i];
@@ -271,23 +298,19 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) bits = v[i].max_bits(bits);
     // every wave's nth largest, then the largest of them that K threads reach
-    const uint32_t key16 = order_key(Vec<TYPE>::max_value(bits)) >> 16, w = threadIdx.x >> 6;
+    const uint32_t key16 = order_key(Vec<TYPE>::max_value(bits)) >> 16;
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u;
     const uint32_t full = min(NW, n / (64 * VEC)), nth = full ? (a.k + full - 1) / full : 64u;
     const uint32_t own = wave_nth16(key16, min(nth, 64u));
-    if ((threadIdx.x & 63u) == 0) sh.bound[w] = own;
+    if (lane == 0) sh.bound[w] = own;
     lds_barrier();
-    uint32_t reached = 0;
-#pragma unroll
-    for (uint32_t i = 0; i < NW; ++i) {
-        const uint32_t c = popc64(ballot(key16 >= sh.bound[i]));
-        reached = (threadIdx.x & 63u) == i ? c : reached;
-    }
-    if ((threadIdx.x & 63u) < NW) atomicAdd(&sh.reached[threadIdx.x & 63u], reached);
-    lds_barrier();
-    uint32_t low = 0;
+    uint32_t reached = 0;  // on lane i: how many of the wave reach wave i's
 #pragma unroll
     for (uint32_t i = 0; i < NW; ++i)
-        if (sh.reached[i] >= a.k) low = max(low, sh.bound[i]);
+        asm("v_writelane_b32 %0, %1, m0" : "+v"(reached) : "s"(popc64(ballot(key16 >= sh.bound[i]))), "{m0}"(i));
+    if (lane < NW) atomicAdd(&sh.reached[lane], reached);
+    lds_barrier();
+    const uint32_t low = lanes_max_u<NW>(sh.reached[lane % NW] >= a.k ? sh.bound[lane % NW] : 0);
     float bound = low ? key16_floor(low) : F_LOWEST;
     // list what reaches the bound, wave by wave, and add the others' exponentials
     const Base2 to2(bound, a.c);
@@ -314,19 +337,15 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
         for (uint32_t e = 0; e < VEC; ++e) sum += to2(x[e]);
         asm volatile("" : "+v"(sum));  // now, not when all vectors' numbers are unpacked
     }
-    if ((threadIdx.x & 63u) == 0) sh.listed[w] = listed;
+    if (lane == 0) sh.listed[w] = listed;
     __syncthreads();
-    uint32_t count = 0, before = 0, equal = 0;
-    bool exact = false;
-#pragma unroll
-    for (uint32_t i = 0; i < NW; ++i) {
-        before = i == w ? count : before;
-        count += sh.listed[i];
-        exact |= sh.listed[i] > WAVE_CAND<NV>;
-    }
-    exact |= count > CAND<NT>;
+    const uint32_t wave_listed = sh.listed[lane % NW], up_to = first_lanes_scan(wave_listed);
+    uint32_t count = __builtin_amdgcn_readlane(up_to, NW - 1), equal = 0;
+    const uint32_t before = __builtin_amdgcn_readlane(up_to, w) - listed;
+    const bool exact = count > CAND<NT> || ballot(wave_listed > WAVE_CAND<NV>) != 0;
     if (!exact)
-        for (uint32_t i = threadIdx.x & 63u; i < listed; i += 64)
+#pragma unroll 1
+        for (uint32_t i = lane; i < listed; i += 64)
             sh.cand[before + i] = top_key(__uint_as_float(wave_cand[w][i].x), start + wave_cand[w][i].y);
     sum = block_sum_f<NT>(sum, sh.red[0]) * to2.to(bound);
     if (exact) {
@@ -355,7 +374,8 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
 // room lets eight blocks share a CU.
 template <uint32_t JT, uint32_t ENTRIES>
 __global__ __launch_bounds__(JT) void k_top_join(TopArgs a) {
-    __shared__ uint64_t in[ENTRIES], sorted[ENTRIES];
+    __shared__ alignas(16) uint64_t in[ENTRIES];
+    __shared__ uint64_t sorted[ENTRIES];
     __shared__ uint32_t ranks[ENTRIES];
     __shared__ float red[3][JT / 64];
     __shared__ uint32_t full, entries;
