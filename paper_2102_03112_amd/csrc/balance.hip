@@ -26,7 +26,8 @@ struct BalanceArgs {
     uint2 *partial;
     uint32_t *prows;
     uint32_t col_blocks;  // joining blocks per group
-    double *gloss;        // sum_e f P per group, or per joining block
+    double *gloss;        // sum_e f P per group, or per joining block,
+    unsigned long long *total;  // or (not null) that of all joining blocks and their number
     int32_t *counts_out, *rows_out;
     float *prob_out, *loss_out;
     // backward
@@ -92,7 +93,7 @@ struct RowBatch {
             for (uint32_t i = 0; i < NI; ++i) {
                 v[u][i].fill_neg_inf();
                 if (valid[u])
-                    v[u][i] = load_vec<TYPE, false>((const typename Num<TYPE>::T *)a.m.p + r * a.m.stride,
+                    v[u][i] = load_vec<TYPE>((const typename Num<TYPE>::T *)a.m.p + r * a.m.stride,
                                                     (i * LANES + sub) * VEC, a.m.cols, row_avail(a.m, r));
             }
         }
@@ -102,9 +103,9 @@ struct RowBatch {
         for (uint32_t i = 0; i < NI * VEC; ++i) x[i] = v[u][i / VEC].get(i % VEC);
     }
 };
-// rows a lane holds at once: 16 to 64 registers
+// rows a lane holds at once: 12 or 16 registers
 template <uint32_t NI>
-constexpr uint32_t ROWS_AT_ONCE = NI == 1 ? 4 : 2;
+constexpr uint32_t ROWS_AT_ONCE = NI == 1 ? 4 : NI == 2 ? 2 : 1;
 
 // One expert's outputs at place i = group E + e; adds count P to the loss.
 __device__ __forceinline__ void put_column(const BalanceArgs &a, uint64_t i, uint32_t count, double p, double &loss) {
@@ -140,6 +141,7 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
     const Rows b = block_rows(a);
     for (uint32_t e = threadIdx.x; e < E; e += BT) hist[e] = 0;
     if (threadIdx.x == 0) rows = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && a.total) *a.total = 0;
     float acc[N] = {};
     uint32_t n = 0;
     for (uint64_t r = b.first + w * RPW + lane / LANES; r - lane / LANES < b.end; r += U * BW * RPW) {
@@ -208,6 +210,24 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
 // loss, too (16384 x 64: 9.9 us in all, and 10.6 with two launches more; of
 // 1024 blocks 17.2 and 14.9).
 constexpr uint32_t JOIN_COLS = 16, ONE_JOIN_COLS = 64;
+
+// The loss from those of up to MAX_ADDING joining blocks, without a launch for
+// it: added as whole numbers of 2^-LOSS_BITS, whose order cannot show, above a
+// count of the blocks, so that one atomic operation adds a block's loss and
+// tells the last one that it is.  A group's sum is at most E <= 2^10, and 2^6
+// blocks have at most that many groups: 2^16 of 2^-36 and a count of 2^6 take
+// 59 bits.  Each such operation on the one word takes some 10 ns, so that more
+// blocks leave their losses to a launch (131072 x 256: 16 blocks 4 us less
+// than with that launch, 512 blocks 5 us more).
+constexpr uint32_t MAX_ADDING = 64, LOSS_BITS = 36, COUNT_BITS = 8;
+__device__ __forceinline__ void add_loss(const BalanceArgs &a, double loss) {
+    constexpr double ONE = (double)(1ull << LOSS_BITS);
+    const unsigned long long add = (unsigned long long)(loss * ONE + 0.5) << COUNT_BITS | 1u;
+    const unsigned long long sum = atomicAdd(a.total, add) + add;
+    if ((sum & ((1u << COUNT_BITS) - 1)) == gridDim.x)
+        a.loss_out[0] = (float)(a.coef / (double)a.r.groups * ((double)(sum >> COUNT_BITS) / ONE));
+}
+
 template <uint32_t JT, uint32_t JOIN_COLS>
 __global__ __launch_bounds__(JT) void k_balance_join(BalanceArgs a) {
     constexpr uint32_t JOIN_WAYS = JT / JOIN_COLS;
@@ -251,6 +271,8 @@ __global__ __launch_bounds__(JT) void k_balance_join(BalanceArgs a) {
         loss *= group_factor(a, n);
         if (gridDim.x == 1)
             a.loss_out[0] = (float)(a.coef * loss);
+        else if (a.total)
+            add_loss(a, loss);
         else
             a.gloss[blockIdx.x] = loss;
     }
@@ -302,30 +324,39 @@ __global__ __launch_bounds__(BT) void k_balance_grad(BalanceArgs a) {
 #pragma unroll
                 for (uint32_t i = 0; i < NI; ++i) {
                     const uint32_t e = (i * LANES + sub) * VEC;
-                    if (e < E) store_vec<TYPE, false>((T *)a.grad + r * a.grad_stride, e, E, x + i * VEC);
+                    if (e < E) store_vec<TYPE>((T *)a.grad + r * a.grad_stride, e, E, x + i * VEC);
                 }
             }
         }
     }
 }
 
-constexpr uint32_t MAX_PARTS = 1024;
-
 // How a type's rows lie over lanes, and the blocks that a call takes.
 struct Shape {
     uint32_t lanes, ni, parts, part_rows;
 };
-Shape plan_rows(uint64_t rows, uint32_t experts, uint32_t type, uint32_t group_rows) {
+constexpr uint32_t MAX_PARTS = 1024, MAX_GRAD_PARTS = 4096;
+Shape plan_rows(uint64_t rows, uint32_t experts, uint32_t type, uint32_t group_rows, bool grad) {
     Shape s;
     const uint32_t vec = 16 / type_bytes(type), vecs = (experts + vec - 1) / vec;
+    // Forward: eight lanes, a line of 128 bytes, for up to four vectors each, so
+    // that exchanges between lanes serve several rows at once (262144 x 256
+    // bfloat16: 41 us, 45 with a lane per vector).  Backward: a lane per vector up
+    // to 64 (58 us, and 77 by eight lanes, whose stores come in more pieces).
     s.lanes = 1;
-    while (s.lanes < 64 && s.lanes < vecs) s.lanes *= 2;
-    s.ni = (vecs + 63) / 64;
+    while (grad ? s.lanes < 64 && s.lanes < vecs : s.lanes < 8 ? s.lanes < vecs : s.lanes * 4 < vecs) s.lanes *= 2;
+    s.ni = (vecs + s.lanes - 1) / s.lanes;
     const uint64_t groups = rows ? (rows + group_rows - 1) / group_rows : 0;
     const uint64_t own = std::min<uint64_t>(rows, group_rows), step = BW * (64 / s.lanes);
-    // four blocks per CU in all, but two rounds of a block's waves at least
-    uint64_t parts = std::max<uint64_t>(1, MAX_PARTS / std::max<uint64_t>(1, groups));
-    parts = std::max<uint64_t>(1, std::min(parts, own / (2 * step)));
+    // Four blocks per CU in all, whose sums are to be joined, but two rounds of a
+    // block's waves at least.  Backward, where there is nothing to join, up to four
+    // times as many, which take turns to load and to store, if they have eight
+    // rounds each, so that f is worth its reading (131072 x 256 fp32: 48 us, 57
+    // with 1024 blocks; 65536 x 256 bfloat16: 17, and 27 as blocks of two rounds).
+    const auto blocks = [&](uint64_t most, uint64_t rounds) {
+        return std::max<uint64_t>(1, std::min(most / std::max<uint64_t>(1, groups), own / (rounds * step)));
+    };
+    const uint64_t parts = grad ? std::max(blocks(MAX_PARTS, 2), blocks(MAX_GRAD_PARTS, 8)) : blocks(MAX_PARTS, 2);
     const uint64_t per = own ? (own + parts - 1) / parts : 1;
     s.part_rows = (uint32_t)((per + step - 1) / step * step);
     s.parts = (uint32_t)std::max<uint64_t>(1, (own + s.part_rows - 1) / s.part_rows);
@@ -334,27 +365,42 @@ Shape plan_rows(uint64_t rows, uint32_t experts, uint32_t type, uint32_t group_r
 
 template <uint32_t TYPE, bool GRAD, uint32_t LANES, uint32_t NI>
 void rows_kernel(const BalanceArgs &a, uint32_t grid, hipStream_t s) {
-    if (GRAD)
+    if constexpr (GRAD)
         k_balance_grad<TYPE, LANES, NI><<<grid, BT, 0, s>>>(a);
     else
         k_balance_rows<TYPE, LANES, NI><<<grid, BT, 0, s>>>(a);
     trace_mark(s, GRAD ? "k_balance_grad" : "k_balance_rows");
 }
 
+// MAX_EXPERTS of 16 bits are 128 vectors, of 32 bits 256
 template <uint32_t TYPE, bool GRAD>
 void rows_launch(const BalanceArgs &a, const Shape &sh, hipStream_t s) {
-    const uint32_t grid = a.r.groups * sh.parts;
-    switch (sh.lanes) {
-        case 1: return rows_kernel<TYPE, GRAD, 1, 1>(a, grid, s);
-        case 2: return rows_kernel<TYPE, GRAD, 2, 1>(a, grid, s);
-        case 4: return rows_kernel<TYPE, GRAD, 4, 1>(a, grid, s);
-        case 8: return rows_kernel<TYPE, GRAD, 8, 1>(a, grid, s);
-        case 16: return rows_kernel<TYPE, GRAD, 16, 1>(a, grid, s);
-        case 32: return rows_kernel<TYPE, GRAD, 32, 1>(a, grid, s);
+    const uint32_t grid = a.r.groups * sh.parts, shape = sh.lanes * 8 + sh.ni;
+    switch (shape) {
+        case 1 * 8 + 1: return rows_kernel<TYPE, GRAD, 1, 1>(a, grid, s);
+        case 2 * 8 + 1: return rows_kernel<TYPE, GRAD, 2, 1>(a, grid, s);
+        case 4 * 8 + 1: return rows_kernel<TYPE, GRAD, 4, 1>(a, grid, s);
+        case 8 * 8 + 1: return rows_kernel<TYPE, GRAD, 8, 1>(a, grid, s);
     }
-    if (sh.ni == 1) return rows_kernel<TYPE, GRAD, 64, 1>(a, grid, s);
-    if (sh.ni == 2) return rows_kernel<TYPE, GRAD, 64, 2>(a, grid, s);
-    if constexpr (TYPE == TYPE_F32) {  // up to MAX_EXPERTS of 4 a vector
+    if constexpr (GRAD) {
+        switch (shape) {
+            case 16 * 8 + 1: return rows_kernel<TYPE, true, 16, 1>(a, grid, s);
+            case 32 * 8 + 1: return rows_kernel<TYPE, true, 32, 1>(a, grid, s);
+            case 64 * 8 + 1: return rows_kernel<TYPE, true, 64, 1>(a, grid, s);
+            case 64 * 8 + 2: return rows_kernel<TYPE, true, 64, 2>(a, grid, s);
+        }
+    } else {
+        switch (shape) {
+            case 8 * 8 + 2: return rows_kernel<TYPE, false, 8, 2>(a, grid, s);
+            case 8 * 8 + 3: return rows_kernel<TYPE, false, 8, 3>(a, grid, s);
+            case 8 * 8 + 4: return rows_kernel<TYPE, false, 8, 4>(a, grid, s);
+            case 16 * 8 + 3: return rows_kernel<TYPE, false, 16, 3>(a, grid, s);
+            case 16 * 8 + 4: return rows_kernel<TYPE, false, 16, 4>(a, grid, s);
+            case 32 * 8 + 3: return rows_kernel<TYPE, false, 32, 3>(a, grid, s);
+            case 32 * 8 + 4: return rows_kernel<TYPE, false, 32, 4>(a, grid, s);
+        }
+    }
+    if constexpr (TYPE == TYPE_F32) {
         if (sh.ni == 3) return rows_kernel<TYPE, GRAD, 64, 3>(a, grid, s);
         return rows_kernel<TYPE, GRAD, 64, 4>(a, grid, s);
     }
@@ -392,19 +438,22 @@ size_t balance_ws_bytes(uint64_t rows, uint64_t experts) {
 
 uint64_t balance_threads(const Matrix &m, const Routes &r) {
     const uint64_t joining = (uint64_t)r.groups * ((m.cols + JOIN_COLS - 1) / JOIN_COLS) * 512;
-    const Shape sh = plan_rows(m.rows, m.cols, m.type, r.group_rows);
-    return std::max((uint64_t)r.groups * sh.parts * BT, sh.parts > 1 ? joining : 0);
+    const Shape sh = plan_rows(m.rows, m.cols, m.type, r.group_rows, false);
+    const Shape gr = plan_rows(m.rows, m.cols, m.type, r.group_rows, true);
+    return std::max((uint64_t)r.groups * std::max(sh.parts, gr.parts) * BT, sh.parts > 1 ? joining : 0);
 }
 
 hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, int32_t *counts_out,
                                   int32_t *rows_out, float *prob_out, float *loss_out, uint8_t *ws, hipStream_t s) {
-    const Shape sh = plan_rows(m.rows, m.cols, m.type, r.group_rows);
+    const Shape sh = plan_rows(m.rows, m.cols, m.type, r.group_rows, false);
     BalanceArgs a = balance_args(m, r, coef, sh);
     const uint64_t blocks = (uint64_t)r.groups * sh.parts;
     a.gloss = (double *)ws;
     const bool one = r.groups == 1 && m.cols <= ONE_JOIN_COLS && sh.parts <= 256;
     a.col_blocks = one ? 1 : (m.cols + JOIN_COLS - 1) / JOIN_COLS;
-    a.partial = (uint2 *)(a.gloss + (sh.parts > 1 ? r.groups * a.col_blocks : r.groups));
+    const uint32_t losses = sh.parts > 1 ? r.groups * a.col_blocks : r.groups;
+    a.total = sh.parts > 1 && losses > 1 && losses <= MAX_ADDING ? (unsigned long long *)ws : nullptr;
+    a.partial = (uint2 *)(a.gloss + losses);
     a.prows = (uint32_t *)(a.partial + blocks * m.cols);
     a.counts_out = counts_out;
     a.rows_out = rows_out;
@@ -414,16 +463,14 @@ hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, 
         hipError_t e = rows_dispatch<false>(a, sh, s);
         if (e != hipSuccess) return e;
     }
-    uint32_t losses = r.groups;
     if (sh.parts > 1) {
-        losses *= a.col_blocks;
         if (one)
             k_balance_join<1024, ONE_JOIN_COLS><<<1, 1024, 0, s>>>(a);
         else
             k_balance_join<512, JOIN_COLS><<<losses, 512, 0, s>>>(a);
         trace_mark(s, "k_balance_join");
     }
-    if (losses != 1) {
+    if (losses != 1 && !a.total) {
         k_balance_mean<<<1, BT, 0, s>>>(a, losses);
         trace_mark(s, "k_balance_mean");
     }
@@ -434,7 +481,7 @@ hipError_t launch_balance_backward(const Matrix &m, const Routes &r, float coef,
                                    const int32_t *count_rows, const int32_t *rows_in, const float *upstream,
                                    void *grad, uint64_t grad_stride, hipStream_t s) {
     if (!r.groups) return hipSuccess;
-    const Shape sh = plan_rows(m.rows, m.cols, m.type, r.group_rows);
+    const Shape sh = plan_rows(m.rows, m.cols, m.type, r.group_rows, true);
     BalanceArgs a = balance_args(m, r, coef, sh);
     a.counts = counts;
     a.count_rows = count_rows;
