@@ -433,6 +433,19 @@ def test_balance(T, E, k, group, dtype):
     check_balance(z.cuda(), experts if E % 2 else experts.int(), mask, group, coef, torch.tensor([0.7]))
 
 
+# every way that a row's vectors lie over lanes; one group, and several of which each has blocks of its own
+@pytest.mark.parametrize("dtype", R.TYPES)
+@pytest.mark.parametrize("group", [611, 150])
+@pytest.mark.parametrize("E", [40, 90, 120, 180, 250, 380, 500, 700, 768, 1000])
+def test_balance_layouts(E, group, dtype):
+    log("balance layouts", E, group, dtype)
+    gen = torch.Generator().manual_seed(E + group)
+    z = (1.5 * torch.randn(611, E, generator=gen)).to(dtype)
+    experts = torch.topk(z.float() + torch.randn(E, generator=gen), 4, 1).indices
+    coef = 100.0 if dtype == torch.float16 else 0.01
+    check_balance(z.cuda(), experts, torch.rand(611, generator=gen) < 0.9, group, coef, torch.tensor([0.7]))
+
+
 @pytest.mark.parametrize("dtype", R.TYPES)
 def test_balance_masks(dtype):
     """Padding that holds NaN, whole groups of padding, masked experts, rows without any expert."""
