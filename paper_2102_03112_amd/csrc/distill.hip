@@ -81,6 +81,9 @@ __device__ __forceinline__ float2 slice_again(const typename Num<TYPE>::T *p, ui
     return make_float2(mx, sum);
 }
 
+// One slice by one block, held in registers from one read: maximum, then sum.
+// Bound by memory: 1500 x 100003 float16: 47 us, 6.4 TB/s; the vector
+// instructions alone take 27.
 template <uint32_t TYPE, int NV>
 __global__ __launch_bounds__(DIST_THREADS) void k_distill_slice(DistillArgs a) {
     using N = Num<TYPE>;
@@ -190,7 +193,8 @@ __device__ __forceinline__ RowResult row_result(float m_tail, double tail, uint3
     return r;
 }
 
-// One wave per row joins its slices; NK entries per lane.
+// One wave per row joins its slices; NK entries per lane.  Bound by latency (an
+// index, then the logit it names): 6.5 us for 1500 rows of 100 entries, 3.7 for 16.
 template <uint32_t TYPE, int NK>
 __global__ __launch_bounds__(DIST_THREADS) void k_distill_join(DistillArgs a) {
     const uint32_t lane = threadIdx.x & 63u;
@@ -246,6 +250,9 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_join(DistillArgs a) {
     }
 }
 
+// The gradient of one slice by one block: f exp2(z c - R) everywhere, then the
+// kept columns.  Bound by memory: 2048 x 65536 bfloat16: 95 us, 5.6 TB/s read and
+// written; the vector instructions alone take 23.
 template <uint32_t TYPE, int NV>
 __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
     using N = Num<TYPE>;
@@ -320,7 +327,10 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
 // beside the memory: 256 CUs hold at most 512 rows at a time, 128 MiB of 131072
 // 16-bit numbers, and it holds 256.  A CU's blocks are rarely in one phase, so
 // that one loads and stores while another adds.  The sum is relative to the
-// largest kept logit, which is known before the row has arrived.
+// largest kept logit, which is known before the row has arrived.  Bound by
+// memory: 4096 x 131072 bfloat16: 405 us, 5.1 TB/s of the logits' and the
+// gradient's bytes; the vector instructions alone take 171.  Short rows by their
+// latency: 256 x 32000 fp32, one row per CU: 15.5 us.
 constexpr int RES = 8;
 
 // Adds a run's numbers but for the kept columns, relative to a reference, and

@@ -280,6 +280,14 @@ __device__ __forceinline__ float2 sum_below(const SliceView<TYPE, NT> &sl, float
     return make_float2(mx, block_sum_f<NT>(sum, red[1]));
 }
 
+// One slice by one block.  A number costs six issue slots (unpack, compare,
+// multiply-add, an exponential at half rate, add), the slice itself (bound,
+// list, ranks) some 300 instructions a wave: so slices are as long as eight
+// vectors a thread allow, at 54 registers, where a SIMD still holds eight waves
+// (16 vectors were slower, and so were blocks of 256 and 1024 threads for long
+// rows).  Bound by vector issue beside memory: 2048 x 131072 bfloat16, K 64: 101
+// us, 5.4 TB/s, of which the vector instructions alone take 84; 777 x 50001
+// fp32, K 100: 37 us, 4.2 TB/s and 25.  8 x 32000: 8 us, one block's latency.
 template <uint32_t TYPE, int NV, uint32_t NT>
 __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
     using N = Num<TYPE>;
@@ -371,7 +379,8 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
 // full lists the ceil(K / F)-th entries bound the K-th largest of all from
 // below, as the threads' largest do in a slice: only what reaches the smallest
 // of them is ranked.  512 keys are enough for the usual few lists, and their
-// room lets eight blocks share a CU.
+// room lets eight blocks share a CU.  Bound by latency (reads, bound, ranks in
+// turn): 8.8 us for 2048 rows of four lists of 64.
 template <uint32_t JT, uint32_t ENTRIES>
 __global__ __launch_bounds__(JT) void k_top_join(TopArgs a) {
     __shared__ alignas(16) uint64_t in[ENTRIES];
@@ -465,7 +474,7 @@ TopPlan plan_top(uint64_t rows, uint64_t cols, uint32_t k, uint32_t type) {
     // The fewest threads that hold a row and are twice K, if rows fill the chip.
     // Else slices as long as they go, also where rows are few: a slice costs a
     // block much the same whatever its length, and one slice needs no join (8 x
-    // 32000 bfloat16, K 50: 8.3 us as one slice, 13.5 as eight).
+    // 32000 bfloat16, K 50: 7.7 us as one slice, 11.2 as eight).
     const uint32_t vec = 16 / type_bytes(type);
     p.threads = 512;
     for (uint32_t t = 128; t < 512; t *= 2)
