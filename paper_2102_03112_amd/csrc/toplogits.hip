@@ -282,12 +282,12 @@ __device__ __forceinline__ float2 sum_below(const SliceView<TYPE, NT> &sl, float
 
 // One slice by one block.  A number costs six issue slots (unpack, compare,
 // multiply-add, an exponential at half rate, add), the slice itself (bound,
-// list, ranks) some 300 instructions a wave: so slices are as long as eight
-// vectors a thread allow, at 54 registers, where a SIMD still holds eight waves
-// (16 vectors were slower, and so were blocks of 256 and 1024 threads for long
-// rows).  Bound by vector issue beside memory: 2048 x 131072 bfloat16, K 64: 101
-// us, 5.4 TB/s, of which the vector instructions alone take 84; 777 x 50001
-// fp32, K 100: 37 us, 4.2 TB/s and 25.  8 x 32000: 8 us, one block's latency.
+// list, ranks) some 300 instructions a wave: so slices are as long as registers
+// allow (plan_top; blocks of 256 and 1024 threads were slower for long rows).
+// Bound by vector issue beside memory: 2048 x 131072 bfloat16, K 64: 99 us, 5.4
+// TB/s, of which the vector instructions alone take 84.  777 x 50001 fp32, K 100:
+// 32 us, 4.9 TB/s, and 17: 1554 blocks of six waves a SIMD are two rounds and a
+// half.  8 x 32000: 8 us, one block's latency.
 template <uint32_t TYPE, int NV, uint32_t NT>
 __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
     using N = Num<TYPE>;
@@ -448,7 +448,14 @@ void slice_kernel(const TopArgs &a, hipStream_t s) {
         case 3: k_top_slice<TYPE, 3, NT><<<grid, NT, 0, s>>>(a); break;
         case 4: k_top_slice<TYPE, 4, NT><<<grid, NT, 0, s>>>(a); break;
         case 6: k_top_slice<TYPE, 6, NT><<<grid, NT, 0, s>>>(a); break;
-        default: k_top_slice<TYPE, 8, NT><<<grid, NT, 0, s>>>(a); break;
+        case 8: k_top_slice<TYPE, 8, NT><<<grid, NT, 0, s>>>(a); break;
+    }
+    if constexpr (NT == 512) {
+        switch (a.sl.nv) {
+            case 10: k_top_slice<TYPE, 10, NT><<<grid, NT, 0, s>>>(a); break;
+            case 12: k_top_slice<TYPE, 12, NT><<<grid, NT, 0, s>>>(a); break;
+            case 16: k_top_slice<TYPE, 16, NT><<<grid, NT, 0, s>>>(a); break;
+        }
     }
     trace_mark(s, "k_top_slice");
 }
@@ -479,10 +486,22 @@ TopPlan plan_top(uint64_t rows, uint64_t cols, uint32_t k, uint32_t type) {
     p.threads = 512;
     for (uint32_t t = 128; t < 512; t *= 2)
         if (p.threads == 512 && rows >= 512 && 2 * k <= t && cols <= (uint64_t)t * TOP_NV * vec) p.threads = t;
-    p.sl = plan_slices(rows, cols, vec, p.threads, TOP_NV, 1);
-    // vectors that the slices need, of 1, 2, 3, 4, 6 and 8
+    // Ten vectors a thread, at 58 registers, leave a SIMD its eight waves; sixteen,
+    // at 80 and more, pay where a row is then one slice, without a join, and for
+    // 32-bit numbers, of which they hold half as many (1000 x 50001 float16, K 200:
+    // 49 us with sixteen, 65 with eight; 1000 x 40000 bfloat16: 21 with ten, 29 with
+    // eight; 1024 x 131072 fp32: 94 and 101; but 2048 x 131072 bfloat16 by twelve
+    // 109, by eight 101).
+    const uint64_t whole = 512ull * 16 * vec;
+    const uint32_t most = p.threads < 512 ? TOP_NV : type == TYPE_F32 || cols <= whole ? 16 : 10;
+    p.sl = plan_slices(rows, cols, vec, p.threads, most, 1);
+    // vectors that the slices need, of those that there are kernels for
     const uint32_t nv = (p.sl.len + p.threads * vec - 1) / (p.threads * vec);
-    p.sl.nv = nv == 5 ? 6 : nv == 7 ? 8 : nv;
+    for (uint32_t n : {1, 2, 3, 4, 6, 8, 10, 12, 16})
+        if (n >= nv) {
+            p.sl.nv = n;
+            break;
+        }
     p.fan = std::max(2u, TOP_JOIN / k);
     p.lists[0] = p.sl.n > 1 ? p.sl.n : 0;
     p.lists[1] = p.sl.n > p.fan ? (p.sl.n + p.fan - 1) / p.fan : 0;

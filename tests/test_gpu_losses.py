@@ -53,6 +53,20 @@ def test_top_logits(rows, cols, k, dtype):
     check_top((3.0 * torch.randn(rows, cols, generator=gen)).to(dtype).cuda(), k, 0.8 if cols % 2 else 1.0)
 
 
+# slices of every length, full and nearly so, alone in their row and with others
+@pytest.mark.parametrize("dtype", R.TYPES)
+@pytest.mark.parametrize("cols,k", [(18000, 30), (20480, 7), (24577, 100), (32768, 64), (32769, 256), (40960, 50),
+                                    (50257, 200), (65535, 1), (65536, 128), (65537, 128), (98000, 64)])
+def test_top_long_slices(cols, k, dtype):
+    log("top long slices", cols, k, dtype)
+    gen = torch.Generator().manual_seed(cols)
+    z = (3 * torch.randn(4, cols, generator=gen)).to(dtype)
+    z[1, : cols - k // 2] = -math.inf  # fewer than k left, at the row's end
+    z[2] = z[2, 0]
+    z[3, 1000:] = -math.inf
+    check_top(z.cuda(), k, 1.5)
+
+
 @pytest.mark.parametrize("dtype", R.TYPES)
 @pytest.mark.parametrize("kind", ["equal", "few", "zeros", "rising", "falling", "high", "blocks", "peaked", "wide",
                                   "strides"])
