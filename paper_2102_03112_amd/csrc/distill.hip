@@ -381,7 +381,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 || !GRAD ? 8 : 6) void k_dis
     constexpr uint32_t VEC = N::VEC, STEP = THREADS * VEC, CHUNK = RES * STEP;
     constexpr int MORE = THREADS < 512 ? 2 : 4;
     extern __shared__ uint32_t bm[];  // a bit per column, then the kept entries:
-    const uint32_t words = (a.m.cols + 31) / 32;
+    const uint32_t words = row_bitmap_words(a.m.cols, STEP);
     float *const ex = (float *)(bm + words), *const ey = ex + a.t.k;  // student's logit, teacher's
     uint32_t *const ej = (uint32_t *)(ey + a.t.k);                    // and column
     __shared__ float red[4][THREADS / 64];
@@ -565,10 +565,20 @@ uint32_t row_threads(const Matrix &m) {
         if (vecs <= t * RES) return t;
     return vecs <= 2 * 512 * RES ? 512 : 1024;
 }
+// Every thread of a step, also one beyond the row, finds its bits in the bitmap.
+constexpr bool bitmap_holds_steps(uint32_t n, uint32_t threads, uint32_t vec) {
+    const uint32_t step = threads * vec, last = (n - 1) / step * (step / vec) + threads - 1;  // vector of the last thread
+    return (last + 1) * vec <= 32 * row_bitmap_words(n, step);
+}
+static_assert(bitmap_holds_steps(1, 64, 8) && bitmap_holds_steps(512, 64, 8) && bitmap_holds_steps(513, 64, 8) &&
+                  bitmap_holds_steps(1, 64, 4) && bitmap_holds_steps(257, 64, 4) && bitmap_holds_steps(2001, 128, 4) &&
+                  bitmap_holds_steps(16383, 256, 8) && bitmap_holds_steps(32000, 512, 4) &&
+                  bitmap_holds_steps(40001, 512, 8) && bitmap_holds_steps(262143, 1024, 8),
+              "bits of a row's last step");
 template <uint32_t TYPE, bool GRAD>
 void row_kernel(const DistillArgs &a, hipStream_t s) {
     const uint32_t grid = (uint32_t)a.m.rows, threads = row_threads(a.m);
-    const uint32_t lds = 4 * ((a.m.cols + 31) / 32 + 3 * a.t.k);
+    const uint32_t lds = 4 * (row_bitmap_words(a.m.cols, threads * (16 / type_bytes(TYPE))) + 3 * a.t.k);
     if (threads == 64)
         k_distill_row<TYPE, 64, GRAD><<<grid, 64, lds, s>>>(a);
     else if (threads == 128)

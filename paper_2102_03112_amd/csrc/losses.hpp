@@ -457,6 +457,9 @@ struct Teacher {
     uint32_t k, idx_type, val_type;
 };
 constexpr uint32_t DIST_THREADS = 256, DIST_NV = 8;
+// Words of the bitmap of a row of n columns that a block reads `step` columns
+// at a time: a bit for every place of every step, the last one's too.
+constexpr uint32_t row_bitmap_words(uint32_t n, uint32_t step) { return (n + step - 1) / step * (step / 32); }
 size_t distill_ws_bytes(uint64_t rows, uint64_t cols, uint32_t type);
 uint64_t distill_threads(const Matrix &m);  // of the largest launch
 hipError_t launch_distill_forward(const Matrix &m, const Teacher &t, float temperature, const float *weight,
