@@ -417,7 +417,7 @@ __global__ __launch_bounds__(JT) void k_top_join(TopArgs a) {
         if (sorted[i * K + K - 1]) atomicMin((unsigned long long *)&bound, sorted[i * K + nth - 1]);
     __syncthreads();
     const uint64_t least = nth ? bound : 1;
-    float left = 0.f;  // what does not reach the bound returns to the sum, relative to the bound
+    float left = 0.f;  // what does not reach the bound returns to the sum
     const float least_x = key_value(least);
     for (uint32_t i = threadIdx.x; i < lists * K; i += JT) {
         const uint64_t key = sorted[i];
@@ -429,9 +429,20 @@ __global__ __launch_bounds__(JT) void k_top_join(TopArgs a) {
     __syncthreads();
     const uint32_t n = entries;
     left = block_sum_f<JT>(left, red[2]);
+    float left_ref = least_x;
+    if (!(left > 1e-20f)) {  // nothing, or all of it far below the bound: relative to its own largest then
+        float mx = F_NEG_INF;
+        for (uint32_t i = threadIdx.x; i < lists * K; i += JT)
+            if (sorted[i] && sorted[i] < least) mx = fmaxf(mx, key_value(sorted[i]));
+        left_ref = block_max_f<JT>(mx, red[0]);
+        left = 0.f;
+        for (uint32_t i = threadIdx.x; i < lists * K; i += JT)
+            if (sorted[i] && sorted[i] < least) left += exp2_fast((key_value(sorted[i]) - left_ref) * a.c);
+        left = block_sum_f<JT>(left, red[1]);
+    }
     if (left > 0.f) {
-        const float b = fmaxf(ref, least_x);
-        sum = top_rescale(sum, ref, b, a.c) + top_rescale(left, least_x, b, a.c);
+        const float b = fmaxf(ref, left_ref);
+        sum = top_rescale(sum, ref, b, a.c) + top_rescale(left, left_ref, b, a.c);
         ref = b;
     }
     rank_keys<JT>(in, n, ranks, sorted);

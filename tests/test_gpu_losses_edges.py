@@ -24,3 +24,19 @@ def test_distill_short_rows_of_one_entry(cols, dtype):
     log("short rows", cols, dtype)
     z, idx, val, rest = R.student(200, cols, 1, dtype, 211 + cols)
     check_distill(z, idx, val, rest if cols > 1 else None, 1.0)
+
+
+@pytest.mark.parametrize("dtype", R.TYPES)
+@pytest.mark.parametrize("cols,k", [(40_000, 2), (131_072, 8), (200_001, 64), (300_007, 12)])
+@pytest.mark.parametrize("background", [0.0, -math.inf])
+def test_top_rest_far_below_kept_logits_of_every_slice(cols, k, background, dtype):
+    """K high logits spread evenly, so that every slice keeps its share, and the next ones far below them: what the
+    slices' lists hold beyond the K is nearly nothing beside them, and all that the rest is made of."""
+    log("top spread", cols, k, background, dtype)
+    for gap, t in ((100.0, 1.0), (150.0, 1.0), (300.0, 1.0), (30.0, 0.1), (600.0, 2.0)):
+        x = torch.full((3, cols), background)
+        x[:, ((torch.arange(k) + 0.5) * cols / k).long()] = 400.0
+        x[0, 1] = 400.0 - gap
+        x[1, 1], x[1, cols - 1] = 400.0 - gap, 399.0 - gap
+        x[2, torch.arange(k) * (cols // k) + 1] = 400.0 - gap  # one more in every part
+        check_top(x.to(dtype).cuda(), k, t)
