@@ -50,8 +50,8 @@ __device__ __forceinline__ uint32_t kept_bits(const uint32_t *bm, uint32_t i) {
 }
 
 // (maximum, sum) of a slice's columns not kept, formed from x - m, by reading
-// the slice again: where nothing is left, where all lies near the lowest
-// number, or where a maximum of bits was no more than an estimate.
+// the slice again: where nothing is left, or where all lies near the lowest
+// number or the largest.
 template <uint32_t TYPE, uint32_t THREADS>
 __device__ __forceinline__ float2 slice_again(const typename Num<TYPE>::T *p, uint32_t n, uint64_t avail,
                                               const uint32_t *bm, float c, float (*red)[THREADS / 64]) {
@@ -101,16 +101,16 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_slice(DistillArgs a) {
     lds_barrier();
     mark_kept(a.t, row, start, n, a.m.cols, bm);
     lds_barrier();
-    uint32_t bits = Vec<TYPE>::max_bits_none();
+    Largest<TYPE> most;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         if (i * DIST_THREADS * VEC >= n) break;
         const uint32_t b = kept_bits<VEC>(bm, i * DIST_THREADS + threadIdx.x);
         if (b) v[i].mask(b);
         v[i].keep_packed();
-        bits = v[i].max_bits(bits);
+        most.add(v[i]);
     }
-    const float mx = block_max_f<DIST_THREADS>(Vec<TYPE>::max_value(bits), red[0]);
+    const float mx = block_max_f<DIST_THREADS>(most.value(), red[0]);
     const Base2 to2(mx, a.c);
     float sum = 0.f;
 #pragma unroll
@@ -338,7 +338,7 @@ constexpr int RES = 8;
 // i THREADS + thread) VEC.
 template <uint32_t TYPE, uint32_t THREADS, bool MAX, int NV>
 __device__ __forceinline__ float sum_run(Vec<TYPE> (&v)[NV], uint32_t n, uint32_t first, const uint32_t *bm,
-                                         const Base2 &to2, float sum, uint32_t &bits) {
+                                         const Base2 &to2, float sum, Largest<TYPE> &most) {
     constexpr uint32_t VEC = Num<TYPE>::VEC;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -346,7 +346,7 @@ __device__ __forceinline__ float sum_run(Vec<TYPE> (&v)[NV], uint32_t n, uint32_
         const uint32_t b = kept_bits<VEC>(bm, first + i * THREADS + threadIdx.x);
         if (b) v[i].mask(b);
         v[i].keep_packed();
-        if (MAX) bits = v[i].max_bits(bits);
+        if (MAX) most.add(v[i]);
 #pragma unroll
         for (uint32_t e = 0; e < VEC; ++e) sum += to2(v[i].get(e));
         asm volatile("" : "+v"(sum));  // one vector's numbers after the other
@@ -419,17 +419,17 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 || !GRAD ? 8 : 6) void k_dis
     lds_barrier();
     float ref = top > F_NEG_INF ? top : 0.f;
     const Base2 by_top(ref, a.c);
-    uint32_t bits = Vec<TYPE>::max_bits_none();
-    float sum = sum_run<TYPE, THREADS, !GRAD>(v, held, 0, bm, by_top, 0.f, bits);
+    Largest<TYPE> most;
+    float sum = sum_run<TYPE, THREADS, !GRAD>(v, held, 0, bm, by_top, 0.f, most);
 #pragma unroll 1
     for (uint32_t e0 = CHUNK; GRAD && e0 < n; e0 += MORE * STEP) {
         Vec<TYPE> u[MORE];
         load_slice<TYPE, THREADS, MORE, false>(u, p + e0, n - e0, avail - e0);
-        sum = sum_run<TYPE, THREADS, false>(u, n - e0, e0 / VEC, bm, by_top, sum, bits);
+        sum = sum_run<TYPE, THREADS, false>(u, n - e0, e0 / VEC, bm, by_top, sum, most);
     }
     sum = block_sum_f<THREADS>(sum, red[1]);
     if (!GRAD) {  // the saved numbers are relative to the largest logit not kept
-        const float mx = block_max_f<THREADS>(Vec<TYPE>::max_value(bits), red[0]);
+        const float mx = block_max_f<THREADS>(most.value(), red[0]);
         ref = mx > F_NEG_INF ? mx : ref;
     }
     float tail = sum * by_top.to(ref);

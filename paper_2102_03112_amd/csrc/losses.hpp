@@ -66,6 +66,16 @@ __device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
     asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
     return r;
 }
+__device__ __forceinline__ uint32_t max_halves_signed(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("v_pk_max_i16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t min_halves_unsigned(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("v_pk_min_u16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
 
 template <uint32_t TYPE>
 __device__ __forceinline__ float num_float(typename Num<TYPE>::T x) {
@@ -149,30 +159,6 @@ struct Vec {
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) w[i] = TYPE == TYPE_F32 ? N::NEG_INF : N::NEG_INF * 0x10001u;
     }
-    // The largest of the numbers so far and this vector's, kept as bits: a float
-    // for 32-bit numbers, two halves for 16-bit ones.  bfloat16 orders as
-    // float16 does, bit for bit, but for magnitudes from 2^121 on, which read
-    // as NaN and are passed over (or come out as such a number): a maximum that
-    // is only an estimate, which the sums that follow it put to the test.
-    __device__ __forceinline__ uint32_t max_bits(uint32_t m) const {
-        if constexpr (TYPE == TYPE_F32) {
-            const float f = max3(__uint_as_float(m), get(0), get(1));
-            return __float_as_uint(max3(f, get(2), get(3)));
-        } else {
-            return max_halves(max_halves(m, w[0]), max_halves(max_halves(w[1], w[2]), w[3]));
-        }
-    }
-    static __device__ __forceinline__ uint32_t max_bits_none() {
-        return TYPE == TYPE_F32 ? N::NEG_INF : N::NEG_INF * 0x10001u;
-    }
-    static __device__ __forceinline__ float max_value(uint32_t m) {
-        if constexpr (TYPE == TYPE_F32) {
-            return __uint_as_float(m);
-        } else {
-            const float a = num_float<TYPE>((T)m), b = num_float<TYPE>((T)(m >> 16));
-            return a > b ? a : b;
-        }
-    }
     __device__ __forceinline__ void put(const float *x) {
         if constexpr (TYPE == TYPE_F32) {
 #pragma unroll
@@ -186,6 +172,47 @@ struct Vec {
                 else
                     w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, half2_t));
             }
+        }
+    }
+};
+
+// The largest number of some vectors, kept as bits (-inf of none).  32-bit
+// numbers: a float.  float16: two halves.  bfloat16: two halves of each of two
+// kinds, as whole numbers: the largest of the bits with their sign, which is
+// the maximum unless all are negative, and the smallest without, which is the
+// maximum then.  (Read as float16, bfloat16 numbers from 2^121 on would be NaN,
+// and the maximum of such halves no number of the vectors.)
+template <uint32_t TYPE>
+struct Largest {
+    using N = Num<TYPE>;
+    uint32_t w = TYPE == TYPE_F32 ? N::NEG_INF : N::NEG_INF * 0x10001u;
+    uint32_t low = N::NEG_INF * 0x10001u;  // bfloat16 only
+
+    __device__ __forceinline__ void add(const Vec<TYPE> &v) {
+        if constexpr (TYPE == TYPE_F32) {
+            const float f = max3(__uint_as_float(w), v.get(0), v.get(1));
+            w = __float_as_uint(max3(f, v.get(2), v.get(3)));
+        } else if constexpr (TYPE == TYPE_BF16) {
+            w = max_halves_signed(max_halves_signed(w, v.w[0]),
+                                  max_halves_signed(max_halves_signed(v.w[1], v.w[2]), v.w[3]));
+            low = min_halves_unsigned(min_halves_unsigned(low, v.w[0]),
+                                      min_halves_unsigned(min_halves_unsigned(v.w[1], v.w[2]), v.w[3]));
+        } else {
+            w = max_halves(max_halves(w, v.w[0]), max_halves(max_halves(v.w[1], v.w[2]), v.w[3]));
+        }
+    }
+    __device__ __forceinline__ float value() const {
+        using T = typename N::T;
+        if constexpr (TYPE == TYPE_F32) {
+            return __uint_as_float(w);
+        } else {
+            uint32_t a = w & 0xffffu, b = w >> 16;
+            if constexpr (TYPE == TYPE_BF16) {
+                a = a & 0x8000u ? low & 0xffffu : a;
+                b = b & 0x8000u ? low >> 16 : b;
+            }
+            const float x = num_float<TYPE>((T)a), y = num_float<TYPE>((T)b);
+            return x > y ? x : y;
         }
     }
 };

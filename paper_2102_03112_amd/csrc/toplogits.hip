@@ -302,11 +302,11 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
     Vec<TYPE> v[NV];
     load_slice<TYPE, NT>(v, p, n, avail);
     if (threadIdx.x < NW) sh.reached[threadIdx.x] = 0;
-    uint32_t bits = Vec<TYPE>::max_bits_none();
+    Largest<TYPE> most;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) bits = v[i].max_bits(bits);
+    for (int i = 0; i < NV; ++i) most.add(v[i]);
     // every wave's nth largest, then the largest of them that K threads reach
-    const uint32_t key16 = order_key(Vec<TYPE>::max_value(bits)) >> 16;
+    const uint32_t key16 = order_key(most.value()) >> 16;
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u;
     const uint32_t full = min(NW, n / (64 * VEC)), nth = full ? (a.k + full - 1) / full : 64u;
     const uint32_t own = wave_nth16(key16, min(nth, 64u));

@@ -40,3 +40,68 @@ def test_top_rest_far_below_kept_logits_of_every_slice(cols, k, background, dtyp
         x[1, 1], x[1, cols - 1] = 400.0 - gap, 399.0 - gap
         x[2, torch.arange(k) * (cols // k) + 1] = 400.0 - gap  # one more in every part
         check_top(x.to(dtype).cuda(), k, t)
+
+
+LARGE = [2.7e36, 3e36, 5e36, 1e37, 4e37, 4.3e37, 1e38, 3.38e38]
+
+
+@pytest.mark.parametrize("cols,k", [(11, 4), (4500, 64), (70_001, 100)])
+def test_top_of_large_bfloat16(cols, k):
+    """Magnitudes whose bits would be no numbers in float16: rows of one, of several, among ordinary ones, and of
+    either sign."""
+    log("top large", cols, k)
+    gen = torch.Generator().manual_seed(311)
+    size = torch.tensor(LARGE)
+    rows = [torch.full((cols,), s * v) for v in LARGE for s in (1.0, -1.0)]
+    pick = size[torch.randint(0, len(LARGE), (6, cols), generator=gen)]
+    sign = torch.where(torch.rand(6, cols, generator=gen) < 0.5, -1.0, 1.0)
+    small = 3.0 * torch.randn(6, cols, generator=gen)
+    rows += [pick[0], -pick[1], pick[2] * sign[2], torch.where(sign[3] > 0, pick[3], small[3]),
+             torch.where(sign[4] > 0, -pick[4], small[4]), 2.0 ** (120 + 7 * torch.rand(cols, generator=gen))]
+    check_top(torch.stack(rows).to(BF16).cuda(), k)
+
+
+def check_step(z, idx, val, rest, t, size, weight=None):
+    """Losses and gradients of all calls against the definition; size: the magnitude of the logits that the loss is
+    made of, masked ones apart."""
+    loss, grad, loss2, grad2 = run_distill(z.cuda(), idx, val, rest, t, weight)
+    want, g, s = R.distill(z, idx, val, rest, t, weight)
+    w = 1.0 if weight is None else weight.abs().double()
+    bound = w * (2 * R.SUM + 2.0 ** -22 * size / t) + (2 * R.SUM + 2.0 ** -22) * want.abs()
+    for got in (loss, loss2):
+        got = got.double().cpu()
+        inf = torch.isinf(want)
+        assert torch.equal(got[inf], want[inf])
+        assert bool(((got - want).abs()[~inf] <= bound.expand_as(want)[~inf]).all()), (got, want)
+    check_grad(grad, g, s, z.dtype, "backward")
+    check_grad(grad2, g, s, z.dtype, "step")
+
+
+@pytest.mark.parametrize("rows,cols", [(3, 3000), (3, 20_000), (2, 70_001), (130, 20_000)])
+def test_distill_bfloat16_masked_with_large_numbers(rows, cols):
+    """Columns masked with a large negative number, among them the last ones of every thread."""
+    log("distill masked with large", rows, cols)
+    z, idx, val, rest = R.student(rows, cols, 20, BF16, 313)
+    weight = torch.zeros(rows)
+    weight[:3] = 1.0
+    for mask in [-1e9, -1e30] + [-v for v in LARGE] + [torch.finfo(BF16).min]:
+        x = z.clone()
+        kept = torch.zeros(rows, cols, dtype=torch.bool).scatter_(1, idx.long(), True)
+        x[:, -2048:] = torch.where(kept, x, mask)[:, -2048:].to(BF16)
+        x[0] = torch.where(kept[0] | (torch.arange(cols) % 3 == 0), x[0].float(), mask).to(BF16)
+        check_step(x, idx, val, rest, 1.0, 40.0, weight)
+
+
+@pytest.mark.parametrize("cols", [3000, 20_000, 70_001])
+def test_distill_large_bfloat16(cols):
+    """Large numbers on both sides: kept ones, others, all."""
+    log("distill large", cols)
+    gen = torch.Generator().manual_seed(317)
+    for v in LARGE[:6]:
+        z, idx, val, rest = R.student(4, cols, 20, BF16, 319)
+        kept = torch.zeros(4, cols, dtype=torch.bool).scatter_(1, idx.long(), True)
+        z[0, 5 if not kept[0, 5] else 6] = v
+        z[1] = torch.where(kept[1], z[1].float(), -v * (0.5 + 0.5 * torch.rand(cols, generator=gen))).to(BF16)
+        z[2] = torch.where(kept[2], z[2].float(), v * torch.ones(cols)).to(BF16)
+        z[3] = -v
+        check_step(z, idx, val, rest, 1.0, 2 * v)
