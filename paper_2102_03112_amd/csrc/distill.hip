@@ -546,13 +546,18 @@ void grad_kernel(const DistillArgs &a, hipStream_t s) {
 // one and by slices: 64 rows 18 and 14 us, 128 rows 20 and 21, 256 rows 29 and
 // 40; 32 rows of 32000: 9.6 and 10.5.
 constexpr uint32_t ROW_MAX_COLS = 1u << 18;
+constexpr uint64_t row_bytes(uint32_t cols, uint32_t type) { return (uint64_t)cols * type_bytes(type); }
 bool step_by_rows(const Matrix &m) {
-    return m.cols <= ROW_MAX_COLS && (m.rows >= 128 || m.cols * type_bytes(m.type) <= 65536);
+    return m.cols <= ROW_MAX_COLS && (m.rows >= 128 || row_bytes(m.cols, m.type) <= 65536);
 }
 // A forward pass gains by rows of up to 256 threads' registers, being one
 // launch (4000 rows of 8000 bfloat16 columns: 20 us one by one, 24 by slices;
 // of 32000: 55 and 53).
-bool forward_by_rows(const Matrix &m) { return m.cols * type_bytes(m.type) <= 256 * RES * 16; }
+constexpr bool forward_by_rows(uint32_t cols, uint32_t type) { return row_bytes(cols, type) <= 256 * RES * 16; }
+static_assert(!forward_by_rows(1u << 30, TYPE_F32) && !forward_by_rows((1u << 30) + 8192, TYPE_F32) &&
+                  !forward_by_rows(1u << 30, TYPE_BF16) && !forward_by_rows(0x7fffffffu, TYPE_F16) &&
+                  forward_by_rows(8192, TYPE_F32) && !forward_by_rows(16385, TYPE_F16),
+              "rows by their bytes, also where these pass 32 bits");
 
 // Threads per row: as many as hold it in RES vectors each, but 512 up to twice
 // that, where three blocks share a CU and one of 1024 threads would have it for
@@ -623,7 +628,7 @@ hipError_t launch_distill_forward(const Matrix &m, const Teacher &t, float tempe
     a.part = (float2 *)ws;
     a.loss = loss_out;
     a.stats = stats_out;
-    if (forward_by_rows(m))
+    if (forward_by_rows(m.cols, m.type))
         return by_type(m.type, [&](auto type) { row_kernel<decltype(type)::value, false>(a, s); });
     return by_type(m.type, [&](auto type) {
         slice_kernel<decltype(type)::value>(a, s);

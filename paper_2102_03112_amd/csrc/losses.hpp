@@ -25,7 +25,7 @@ constexpr float F_LOWEST = -3.4028234663852886e38f;
 constexpr float F_NEG_INF = -__builtin_inff();
 constexpr uint32_t KEY_NEG_INF = 0x007fffffu;  // order_key(-inf)
 
-inline uint32_t type_bytes(uint32_t type) { return type == TYPE_F32 ? 4u : 2u; }
+constexpr uint32_t type_bytes(uint32_t type) { return type == TYPE_F32 ? 4u : 2u; }
 
 // A matrix of logits (or of gradients) as the kernels take it.
 struct Matrix {

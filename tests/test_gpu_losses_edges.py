@@ -105,3 +105,36 @@ def test_distill_large_bfloat16(cols):
         z[2] = torch.where(kept[2], z[2].float(), v * torch.ones(cols)).to(BF16)
         z[3] = -v
         check_step(z, idx, val, rest, 1.0, 2 * v)
+
+
+def test_distill_row_of_more_than_2_to_the_32_bytes():
+    """One fp32 row of 2^30 and some columns, whose bytes pass 32 bits: loss and gradient against sums in 64 bits."""
+    cols, parts = (1 << 30) + 5, 64
+    gen = torch.Generator(device="cuda").manual_seed(331)
+    z = torch.empty(1, cols, device="cuda")
+    for a in range(0, cols, 1 << 26):
+        n = min(1 << 26, cols - a)
+        z[0, a:a + n] = torch.randn(n, generator=gen, device="cuda")
+    idx = torch.tensor([[3, 1 << 29, cols - 1]], dtype=torch.int32, device="cuda")
+    z[0, idx[0].long()] = torch.tensor([20.0, 19.0, 21.5], device="cuda")
+    val, rest = torch.tensor([[5.0, 4.0, 6.0]], device="cuda"), torch.tensor([4.5], device="cuda")
+    log("2^30 columns")
+    loss, stats = torch.zeros(1, device="cuda"), torch.zeros(1, L.STATS, device="cuda")
+    grad, ws, teacher = torch.empty_like(z), L.workspace(1, cols, 3), L.Teacher(idx, val, rest)
+    L.distill_forward(z, teacher, 1.0, None, loss, stats, ws)
+    L.distill_step(z, teacher, 1.0, None, loss, grad, ws)
+    total = sum(float(torch.exp(c.double()).sum()) for c in torch.chunk(z[0], parts))
+    kept = z[0, idx[0].long()].double().cpu()
+    tail = total - float(torch.exp(kept).sum())
+    p = torch.softmax(torch.cat([val[0], rest]).double().cpu(), 0)
+    q = torch.cat([torch.exp(kept), torch.tensor([tail], dtype=torch.float64)]) / total
+    assert abs(float(loss) - float((p * (torch.log(p) - torch.log(q))).sum())) <= 2 * R.SUM + 2.0 ** -22 * 22
+    got = grad[0, idx[0].long()].double().cpu()
+    assert bool(((got - (q - p)[:3]).abs() <= 2 * R.SUM * (q + p)[:3] + 2.0 ** -23).all())
+    factor = (float(q[3]) - float(p[3])) / tail
+    for a in (0, 4, (1 << 29) + 1, cols - 1001):  # where no column is kept
+        want = torch.exp(z[0, a:a + 1000].double()) * factor
+        if a == 0:
+            want[3] = grad[0, 3].double()
+        bound = 2 * R.SUM * torch.exp(z[0, a:a + 1000].double()) * (float(q[3]) + float(p[3])) / tail
+        assert bool(((grad[0, a:a + 1000].double() - want).abs() <= bound + 2.0 ** -23 * want.abs()).all())
