@@ -433,7 +433,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 || !GRAD ? 8 : 6) void k_dis
         ref = mx > F_NEG_INF ? mx : ref;
     }
     float tail = sum * by_top.to(ref);
-    if (!(sum > 1e-28f && sum < 1e30f && tail < 1e30f)) {
+    if (!(sum > 1e-28f && sum < 1e30f && tail > 1e-30f && tail < 1e30f)) {
         const float2 x = slice_again<TYPE, THREADS>(p, n, avail, bm, a.c, red + 2);
         ref = x.x;
         tail = x.y;

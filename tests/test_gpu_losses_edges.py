@@ -138,3 +138,18 @@ def test_distill_row_of_more_than_2_to_the_32_bytes():
             want[3] = grad[0, 3].double()
         bound = 2 * R.SUM * torch.exp(z[0, a:a + 1000].double()) * (float(q[3]) + float(p[3])) / tail
         assert bool(((grad[0, a:a + 1000].double() - want).abs() <= bound + 2.0 ** -23 * want.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [900, 9000, 20_000])
+def test_distill_where_a_kept_logit_is_large(cols, dtype):
+    """A kept logit so large that no other has a probability: the loss is finite, p_rest times the distance."""
+    log("large kept", cols, dtype)
+    for v in (1e31, 3e36, 1e37):
+        z, idx, val, rest = R.student(130, cols, 20, dtype, 337)
+        z.scatter_(1, idx[:, :1].long(), v)
+        weight = torch.zeros(130)
+        weight[:4] = 1.0
+        z[1] = z[1].float().abs().clamp(max=3.0).to(dtype)  # and one row as usual
+        z[2, idx[2, 1].long()] = v / 2
+        check_step(z, idx, val, rest, 1.0, 40.0, weight)
