@@ -143,31 +143,39 @@ struct RowResult {
 template <typename ENTRY>
 __device__ __forceinline__ RowResult row_result(float m_tail, double tail, uint32_t n, ENTRY entry, float rest, float c,
                                                 float inv_t) {
-    float m_p = rest, m = m_tail, x, y;
+    float y0 = F_NEG_INF, m = m_tail, x, y;
 #pragma unroll
     for (uint32_t i = 0; i < n; ++i)
         if (entry(i, x, y)) {
             m = fmaxf(m, x);
-            m_p = fmaxf(m_p, y * inv_t);
+            y0 = fmaxf(y0, y);
         }
     m = wave_max_f(m);
-    m_p = wave_max_f(m_p);
-    // sums relative to m and m_p; d: the teacher's logit less the student's
+    y0 = wave_max_f(y0);
+    // The teacher's reference: the largest logit over the temperature, or rest.
+    const double y0_t = y0 == F_NEG_INF ? (double)y0 : fmin(fmax((double)y0 * inv_t, (double)F_LOWEST), -(double)F_LOWEST);
+    const float m_p = fmaxf((float)y0_t, rest);
+    // Sums relative to y0 and m; d: the entry's ln of p over q but for the
+    // sums.  Logits are taken off one another before anything else, so that
+    // large ones, a mask's lowest number say, leave no error of their size.
     double sum_q = 0.0, sum_p = 0.0, sum_d = 0.0;
 #pragma unroll
     for (uint32_t i = 0; i < n; ++i) {
         if (!entry(i, x, y)) continue;
         if (x != F_NEG_INF) sum_q += exp2_fast((x - m) * c);
-        const float e = y == F_NEG_INF ? 0.f : exp_below(y * inv_t - m_p);
+        const float e = y == F_NEG_INF ? 0.f : exp2_fast((y - y0) * c);
         if (e > 0.f) {
             sum_p += e;
-            sum_d += e * (((double)y - (double)x) * (double)inv_t);
+            sum_d += e * ((((double)y - (double)y0) - ((double)x - (double)m)) * (double)inv_t);
         }
     }
     const double tail_q = tail == 0.0 ? 0.0 : tail * exp2_fast((m_tail - m) * c);
     sum_q = wave_sum_f64(sum_q) + tail_q;
     sum_p = wave_sum_f64(sum_p);
     sum_d = wave_sum_f64(sum_d);
+    const float y0_p = y0 == F_NEG_INF ? 0.f : exp_below((float)(y0_t - m_p));  // and now relative to m_p
+    sum_d = y0_p > 0.f ? y0_p * (sum_d + (y0_t - m_p) * sum_p) : 0.0;
+    sum_p *= y0_p;
     const float e_rest = rest == F_NEG_INF ? 0.f : exp_below(rest - m_p);
     sum_p += e_rest;
     RowResult r;
@@ -178,9 +186,10 @@ __device__ __forceinline__ RowResult row_result(float m_tail, double tail, uint3
         if (sum_q == 0.0 || (e_rest > 0.f && tail == 0.0)) {
             r.loss = __builtin_inf();
         } else {
-            if (e_rest > 0.f) sum_d += e_rest * ((double)rest - ((double)m_tail * inv_t + ln_sum(tail)));
-            // the terms' mean, less ln of one normaliser over the other
-            r.loss = sum_d / sum_p - ((m_p + ln_sum(sum_p)) - ((double)m * inv_t + ln_sum(sum_q)));
+            if (e_rest > 0.f)
+                sum_d += e_rest * (((double)rest - m_p) - (((double)m_tail - m) * (double)inv_t + ln_sum(tail)));
+            // the terms' mean, less ln of one sum over the other
+            r.loss = sum_d / sum_p - (ln_sum(sum_p) - ln_sum(sum_q));
         }
         if (tail > 0.0) a_tail = (tail_q / sum_q - e_rest / sum_p) / tail;
     }
@@ -191,6 +200,14 @@ __device__ __forceinline__ RowResult row_result(float m_tail, double tail, uint3
     r.stats[4] = m_p;
     r.stats[5] = sum_p > 0.0 ? (float)(1.0 / sum_p) : 0.f;
     return r;
+}
+
+// p of an entry with the teacher's logit y, from the saved reference and 1 /
+// sum.  A quotient below a float's range counts as the range's end, also where
+// that is the reference.
+__device__ __forceinline__ float entry_p(float y, float inv_t, float m_p, float inv_sum) {
+    if (y == F_NEG_INF) return 0.f;
+    return exp_below(m_p == F_LOWEST ? fmaxf(y * inv_t, F_LOWEST) - m_p : fmaf(y, inv_t, -m_p)) * inv_sum;
 }
 
 // One wave per row joins its slices; NK entries per lane.  Bound by latency (an
@@ -289,9 +306,8 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
         const uint32_t j = load_index(a.t.idx, row * a.t.idx_stride + k, a.t.idx_type, a.m.cols) - start;
         if (j >= n) continue;
         const float x = num_float<TYPE>(p[j]), y = load_num(a.t.val, row * a.t.val_stride + k, a.t.val_type);
-        const float e = y == F_NEG_INF ? 0.f : exp_below(y * a.inv_t - st[4]) * st[5];
         at[i] = j;
-        g[i] = q * exp2_fast((x - m) * a.c) - scale * e;
+        g[i] = q * exp2_fast((x - m) * a.c) - scale * entry_p(y, a.inv_t, st[4], st[5]);
     }
     __syncthreads();
     const Base2 to2(m_tail, a.c);
@@ -484,8 +500,8 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 || !GRAD ? 8 : 6) void k_dis
     __syncthreads();  // the kept columns are written again
     for (uint32_t k = threadIdx.x; k < a.t.k; k += THREADS) {
         if (ej[k] >= n) continue;
-        const float e = ey[k] == F_NEG_INF ? 0.f : exp_below(ey[k] * a.inv_t - row_stats[4]) * row_stats[5];
-        out[ej[k]] = num_round<TYPE>(q * exp2_fast((ex[k] - m) * a.c) - scale * e);
+        const float p_k = entry_p(ey[k], a.inv_t, row_stats[4], row_stats[5]);
+        out[ej[k]] = num_round<TYPE>(q * exp2_fast((ex[k] - m) * a.c) - scale * p_k);
     }
 }
 

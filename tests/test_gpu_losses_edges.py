@@ -153,3 +153,23 @@ def test_distill_where_a_kept_logit_is_large(cols, dtype):
         z[1] = z[1].float().abs().clamp(max=3.0).to(dtype)  # and one row as usual
         z[2, idx[2, 1].long()] = v / 2
         check_step(z, idx, val, rest, 1.0, 40.0, weight)
+
+
+@pytest.mark.parametrize("dtype", R.TYPES)
+@pytest.mark.parametrize("values", R.TYPES)
+@pytest.mark.parametrize("cols", [700, 40_000])
+def test_distill_of_rows_masked_with_the_lowest_number(cols, values, dtype):
+    """A whole row of a teacher's, of a student's or of both masked with the type's lowest number is a uniform
+    distribution, and its loss a few nats: no difference of such numbers shows."""
+    log("lowest", cols, values, dtype)
+    low = torch.finfo(values).min
+    for t in (0.7, 1.0, 2.0):
+        z, idx, val, rest = R.student(6, cols, 20, dtype, 347, t)
+        val = val.to(values)
+        val[0], val[1], val[4] = low, low, low
+        val[5, 1:] = low
+        rest[0] = rest[4] = -math.inf
+        rest[1] = low / t if t >= 1.0 else -math.inf  # a float, and the quotient's very number
+        z[2] = z[3] = z[4] = torch.finfo(dtype).min
+        rest[3] = -math.inf
+        check_step(z, idx, val, rest, t, 40.0)
