@@ -104,10 +104,12 @@ DR_EXPORT dr_status dr_top_logits(const dr_logits *logits_h, uint32_t k, float t
  * 1 / n and distillation's customary t^2 into it.  A row of weight 0 is not
  * read at all, whatever it holds: loss, saved numbers and gradient are 0.  A
  * teacher's row without entries has p_rest = q_rest = 1 and loss 0 if its
- * rest is finite, and no distribution, loss 0 and gradient 0 if rest is -inf
- * (or null).  A student's row that gives a kept column no probability (its
- * logit is -inf) has loss +inf and a finite gradient.  One entry per row and
- * rest null is the cross entropy with that column as the label.
+ * rest is finite (+inf if the student's row is all -inf).  Where rest is -inf
+ * or null, a teacher's row without entries, or with logits of -inf alone, is
+ * no distribution, and has loss 0 and gradient 0.  A student's row that gives
+ * a kept column no probability (its logit is -inf) has loss +inf and a finite
+ * gradient.  One entry per row and rest null is the cross entropy with that
+ * column as the label.
  *
  * stats_out (nullable, rows x DR_DISTILL_STATS, contiguous) receives what the
  * backward pass reads: m = the row's largest logit, 1 / S with S = sum_j

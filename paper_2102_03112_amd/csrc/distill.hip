@@ -294,7 +294,8 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
     load_slice<TYPE, DIST_THREADS>(v, p, n, avail);
     const float *st = a.stats + row * STATS;
     const float m = st[0] == F_NEG_INF ? 0.f : st[0], m_tail = st[2] == F_NEG_INF ? 0.f : st[2];
-    const float scale = w * u * a.inv_t, q = scale * st[1], f = scale * st[3];
+    // no gradient where the teacher's row is no distribution
+    const float scale = w * u * a.inv_t, q = st[5] > 0.f ? scale * st[1] : 0.f, f = scale * st[3];
     // the kept columns of this slice: read before any thread writes, written after all have
     uint32_t at[PER];
     float g[PER];
@@ -475,7 +476,8 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 || !GRAD ? 8 : 6) void k_dis
     }
     if constexpr (!GRAD) return;
     lds_barrier();
-    const float m = row_stats[0] == F_NEG_INF ? 0.f : row_stats[0], scale = w * a.inv_t, q = scale * row_stats[1];
+    const float m = row_stats[0] == F_NEG_INF ? 0.f : row_stats[0], scale = w * a.inv_t;
+    const float q = row_stats[5] > 0.f ? scale * row_stats[1] : 0.f;  // no gradient without a teacher's distribution
     ref = ref == F_NEG_INF ? 0.f : ref;
     const Base2 to2(ref, a.c);
     const float f = scale * row_stats[3], f2 = f * to2.to(ref);

@@ -173,3 +173,20 @@ def test_distill_of_rows_masked_with_the_lowest_number(cols, values, dtype):
         z[2] = z[3] = z[4] = torch.finfo(dtype).min
         rest[3] = -math.inf
         check_step(z, idx, val, rest, t, 40.0)
+
+
+@pytest.mark.parametrize("dtype", R.TYPES)
+@pytest.mark.parametrize("rows,cols", [(5, 600), (5, 40_000), (130, 20_000)])
+def test_distill_of_a_teachers_row_of_minus_infinity(rows, cols, dtype):
+    """Entries whose logits are all -inf, and no rest: no distribution, loss 0 and gradient 0, as without entries."""
+    z, idx, val, rest = R.student(rows, cols, 20, dtype, 349)
+    weight = torch.zeros(rows)
+    weight[:5] = 1.0
+    val[1], rest[1] = -math.inf, -math.inf
+    val[2, 3:], rest[2] = -math.inf, -math.inf
+    val[3] = -math.inf
+    idx[4], rest[4] = -1, -math.inf
+    check_step(z, idx, val, rest, 1.0, 40.0, weight)
+    loss, grad, loss2, grad2 = run_distill(z.cuda(), idx, val, rest, 1.0, weight)
+    for x in (loss, loss2, grad, grad2):
+        assert float(x[[1, 4]].abs().max()) == 0.0
