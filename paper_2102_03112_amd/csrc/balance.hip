@@ -26,8 +26,8 @@ struct BalanceArgs {
     uint2 *partial;
     uint32_t *prows;
     uint32_t col_blocks;  // joining blocks per group
-    double *gloss;        // sum_e f P per group, or per joining block,
-    unsigned long long *total;  // or (not null) that of all joining blocks and their number
+    double *gloss;        // sum_e f P per group, or per joining block
+    uint32_t *done;       // not null: the joining blocks that have left theirs
     int32_t *counts_out, *rows_out;
     float *prob_out, *loss_out;
     // backward
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
     const Rows b = block_rows(a);
     for (uint32_t e = threadIdx.x; e < E; e += BT) hist[e] = 0;
     if (threadIdx.x == 0) rows = 0;
-    if (blockIdx.x == 0 && threadIdx.x == 0 && a.total) *a.total = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && a.done) *a.done = 0;
     float acc[N] = {};
     uint32_t n = 0;
     for (uint64_t r = b.first + w * RPW + lane / LANES; r - lane / LANES < b.end; r += U * BW * RPW) {
@@ -215,20 +215,27 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
 constexpr uint32_t JOIN_COLS = 16, ONE_JOIN_COLS = 64;
 
 // The loss from those of up to MAX_ADDING joining blocks, without a launch for
-// it: added as whole numbers of 2^-LOSS_BITS, whose order cannot show, above a
-// count of the blocks, so that one atomic operation adds a block's loss and
-// tells the last one that it is.  A group's sum is at most E <= 2^10, and 2^6
-// blocks have at most that many groups: 2^16 of 2^-36 and a count of 2^6 take
-// 59 bits.  Each such operation on the one word takes some 10 ns, so that more
-// blocks leave their losses to a launch (131072 x 256: 16 blocks 4 us less
-// than with that launch, 512 blocks 5 us more).
-constexpr uint32_t MAX_ADDING = 64, LOSS_BITS = 36, COUNT_BITS = 8;
-__device__ __forceinline__ void add_loss(const BalanceArgs &a, double loss) {
-    constexpr double ONE = (double)(1ull << LOSS_BITS);
-    const unsigned long long add = (unsigned long long)(loss * ONE + 0.5) << COUNT_BITS | 1u;
-    const unsigned long long sum = atomicAdd(a.total, add) + add;
-    if ((sum & ((1u << COUNT_BITS) - 1)) == gridDim.x)
-        a.loss_out[0] = (float)(a.coef / (double)a.r.groups * ((double)(sum >> COUNT_BITS) / ONE));
+// it: each leaves its own and then counts itself, and the last one that does
+// adds them, in 64 bits and in their order.  All of it by atomic operations,
+// which take place where every block sees them; one that returns is done, and
+// so the count's operand is made from what leaving the loss returned.  Each
+// operation on the one count takes some 10 ns, so that more blocks leave their
+// losses to a launch.
+constexpr uint32_t MAX_ADDING = 64;
+__device__ __forceinline__ void add_losses(const BalanceArgs &a, double loss) {  // the first wave; loss: lane 0's
+    auto *const left = (unsigned long long *)a.gloss;
+    const uint32_t lane = threadIdx.x;
+    uint32_t last = 0;
+    if (lane == 0) {
+        const unsigned long long was = atomicExch(&left[blockIdx.x], __builtin_bit_cast(unsigned long long, loss));
+        uint32_t one;
+        asm volatile("v_mov_b32 %0, 1" : "=v"(one) : "v"((uint32_t)was));
+        last = atomicAdd(a.done, one) + 1 == gridDim.x ? 1u : 0u;
+    }
+    if (!__builtin_amdgcn_readfirstlane(last)) return;
+    double sum = lane < gridDim.x ? __builtin_bit_cast(double, atomicAdd(&left[lane], 0ull)) : 0.0;
+    sum = wave_sum_f64(sum);
+    if (lane == 0) a.loss_out[0] = (float)(a.coef / (double)a.r.groups * sum);
 }
 
 template <uint32_t JT, uint32_t JOIN_COLS>
@@ -268,17 +275,15 @@ __global__ __launch_bounds__(JT) void k_balance_join(BalanceArgs a) {
         }
         if (e < E) put_column(a, (uint64_t)g * E + e, c, n ? s / n : 0.0, loss);
     }
-    loss = block_loss<JT>(loss, red);
+    loss = block_loss<JT>(loss, red) * group_factor(a, n);
     if (threadIdx.x == 0) {
         if (blockIdx.x % a.col_blocks == 0) a.rows_out[g] = (int32_t)n;
-        loss *= group_factor(a, n);
         if (gridDim.x == 1)
             a.loss_out[0] = (float)(a.coef * loss);
-        else if (a.total)
-            add_loss(a, loss);
-        else
+        else if (!a.done)
             a.gloss[blockIdx.x] = loss;
     }
+    if (a.done && threadIdx.x < 64) add_losses(a, loss);
 }
 
 // The mean over groups, from n parts of their losses: a launch's 4.4 us.
@@ -435,10 +440,10 @@ BalanceArgs balance_args(const Matrix &m, const Routes &r, float coef, const Sha
 }  // namespace
 
 // Results are kept per block where groups have several (at most MAX_PARTS
-// blocks then), and losses per group or per joining block.
+// blocks then), and losses per group or per joining block, behind a count.
 size_t balance_ws_bytes(uint64_t rows, uint64_t experts) {
     const uint64_t joining = MAX_PARTS / 2 * ((experts + JOIN_COLS - 1) / JOIN_COLS);
-    return 8 * std::max<uint64_t>(rows, joining) + MAX_PARTS * (8 * experts + 4);
+    return 8 + 8 * std::max<uint64_t>(rows, joining) + MAX_PARTS * (8 * experts + 4);
 }
 
 uint64_t balance_threads(const Matrix &m, const Routes &r) {
@@ -453,11 +458,11 @@ hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, 
     const Shape sh = plan_rows(m.rows, m.cols, m.type, r.group_rows, false);
     BalanceArgs a = balance_args(m, r, coef, sh);
     const uint64_t blocks = (uint64_t)r.groups * sh.parts;
-    a.gloss = (double *)ws;
+    a.gloss = (double *)(ws + 8);
     const bool one = r.groups == 1 && m.cols <= ONE_JOIN_COLS && sh.parts <= 256;
     a.col_blocks = one ? 1 : (m.cols + JOIN_COLS - 1) / JOIN_COLS;
     const uint32_t losses = sh.parts > 1 ? r.groups * a.col_blocks : r.groups;
-    a.total = sh.parts > 1 && losses > 1 && losses <= MAX_ADDING ? (unsigned long long *)ws : nullptr;
+    a.done = sh.parts > 1 && losses > 1 && losses <= MAX_ADDING ? (uint32_t *)ws : nullptr;
     a.partial = (uint2 *)(a.gloss + losses);
     a.prows = (uint32_t *)(a.partial + blocks * m.cols);
     a.counts_out = counts_out;
@@ -475,7 +480,7 @@ hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, 
             k_balance_join<512, JOIN_COLS><<<losses, 512, 0, s>>>(a);
         trace_mark(s, "k_balance_join");
     }
-    if (losses != 1 && !a.total) {
+    if (losses != 1 && !a.done) {
         k_balance_mean<<<1, BT, 0, s>>>(a, losses);
         trace_mark(s, "k_balance_mean");
     }

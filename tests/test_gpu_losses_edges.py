@@ -190,3 +190,31 @@ def test_distill_of_a_teachers_row_of_minus_infinity(rows, cols, dtype):
     loss, grad, loss2, grad2 = run_distill(z.cuda(), idx, val, rest, 1.0, weight)
     for x in (loss, loss2, grad, grad2):
         assert float(x[[1, 4]].abs().max()) == 0.0
+
+
+# one block, one joining block, 3 .. 64 of them, and more
+BALANCE_ROUTES = [(60, 8, 60), (4000, 64, 4000), (4000, 200, 4000), (6000, 40, 2000), (4000, 256, 1000),
+                  (3000, 1000, 3000), (9000, 256, 900)]
+
+
+@pytest.mark.parametrize("dtype", R.TYPES)
+@pytest.mark.parametrize("gap", [4.0, 14.0, 30.0, 60.0])
+@pytest.mark.parametrize("T,E,group", BALANCE_ROUTES)
+def test_balance_loss_of_improbable_choices(T, E, group, gap, dtype):
+    """Experts chosen whose probability is next to nothing: a loss far below 1, as exact as any other."""
+    log("improbable", T, E, group, gap, dtype)
+    gen = torch.Generator().manual_seed(353)
+    z = torch.randn(T, E, generator=gen)
+    z[:, E // 2:] -= gap
+    experts = torch.randint(E // 2, E, (T, 2), generator=gen)
+    check_balance(z.to(dtype).cuda(), experts, None, group, 1.0)
+
+
+@pytest.mark.parametrize("T,E,group", BALANCE_ROUTES)
+def test_balance_loss_shows_a_nan(T, E, group):
+    """A router that has gone NaN has no finite loss, whichever blocks join it."""
+    gen = torch.Generator().manual_seed(359)
+    z = torch.randn(T, E, generator=gen)
+    z[T // 2, 3] = math.nan
+    experts = torch.randint(0, E, (T, 2), generator=gen)
+    assert math.isnan(float(run_balance(z.cuda(), experts, None, group, 1.0)[3]))
