@@ -132,11 +132,14 @@ __device__ __forceinline__ double group_factor(const BalanceArgs &a, uint32_t n)
 // Sums and counts of a block's rows.  Bound by memory where rows are many: 131072
 // x 256 fp32: 27 us, 5.1 TB/s; the vector instructions alone take 14.  Else by
 // latency (load, softmax, counts in turn): 16384 x 64 bfloat16: 5.3 us.
+// A lane adds FOLD rows in 32 bits, and what these give in 64: blocks of groups
+// that are many and long have thousands of rows a lane.
+constexpr uint32_t FOLD = 64;
 template <uint32_t TYPE, uint32_t LANES, uint32_t NI>
 __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
     constexpr uint32_t VEC = Num<TYPE>::VEC, N = NI * VEC, RPW = 64 / LANES, COLS = LANES * N;
     constexpr uint32_t U = ROWS_AT_ONCE<NI>;
-    __shared__ float sums[BW][COLS];
+    __shared__ double sums[BW][COLS];
     __shared__ uint32_t hist[MAX_EXPERTS];
     __shared__ uint32_t rows;
     __shared__ double red[BW];
@@ -146,7 +149,18 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
     if (threadIdx.x == 0) rows = 0;
     if (blockIdx.x == 0 && threadIdx.x == 0 && a.done) *a.done = 0;
     float acc[N] = {};
-    uint32_t n = 0;
+    uint32_t n = 0, added = 0;
+    bool folded = false;
+    const auto fold = [&] {  // the wave's rows; its own lanes' sums
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) {
+            const float x = groups_sum<LANES>(acc[i]);
+            double &s = sums[w][(i / VEC * LANES + sub) * VEC + i % VEC];
+            if (lane < LANES) s = folded ? s + x : x;
+            acc[i] = 0.f;
+        }
+        folded = true;
+    };
     for (uint64_t r = b.first + w * RPW + lane / LANES; r - lane / LANES < b.end; r += U * BW * RPW) {
         RowBatch<TYPE, LANES, NI, U> rows_now;
         rows_now.load(a, r, b.end, BW * RPW, sub);
@@ -160,13 +174,13 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
 #pragma unroll
             for (uint32_t i = 0; i < N; ++i) acc[i] += x[i];
         }
+        added += U;
+        if (added == FOLD) {
+            fold();
+            added = 0;
+        }
     }
-#pragma unroll
-    for (uint32_t i = 0; i < N; ++i) acc[i] = groups_sum<LANES>(acc[i]);  // the wave's rows
-    if (lane < LANES) {
-#pragma unroll
-        for (uint32_t i = 0; i < N; ++i) sums[w][(i / VEC * LANES + sub) * VEC + i % VEC] = acc[i];
-    }
+    fold();
     n = wave_sum(n);
     lds_barrier();
     if (lane == 0 && n) atomicAdd(&rows, n);
@@ -182,11 +196,11 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
     const double inv = rows ? 1.0 / rows : 0.0;
     double loss = 0.0;
     for (uint32_t e = threadIdx.x; e < E; e += BT) {
-        float s = sums[0][e];
+        double s = sums[0][e];
 #pragma unroll
         for (uint32_t i = 1; i < BW; ++i) s += sums[i][e];
         if (a.parts > 1) {
-            a.partial[at + e] = make_uint2(__float_as_uint(s), hist[e]);
+            a.partial[at + e] = make_uint2(__float_as_uint((float)s), hist[e]);
         } else {
             put_column(a, at + e, hist[e], s * inv, loss);
         }

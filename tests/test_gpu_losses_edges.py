@@ -218,3 +218,45 @@ def test_balance_loss_shows_a_nan(T, E, group):
     z[T // 2, 3] = math.nan
     experts = torch.randint(0, E, (T, 2), generator=gen)
     assert math.isnan(float(run_balance(z.cuda(), experts, None, group, 1.0)[3]))
+
+
+def test_balance_of_many_long_groups():
+    """More than 512 groups have a block each, whose lanes add thousands of rows: equal logits, so that every one of
+    those additions rounds the same way."""
+    group, E, G = 4096 * 128, 5, 513
+    log("long groups")
+    z = torch.zeros(group * G, E, device="cuda")
+    experts = torch.zeros(group * G, 1, dtype=torch.int32, device="cuda")
+    counts, n = torch.zeros(G, E, dtype=torch.int32, device="cuda"), torch.zeros(G, dtype=torch.int32, device="cuda")
+    prob, loss = torch.zeros(G, E, device="cuda"), torch.zeros(1, device="cuda")
+    L.balance_forward(z, experts, None, group, 1.0, counts, n, prob, loss, L.workspace(group * G, E, 1))
+    assert bool((counts[:, 0] == group).all()) and bool((n == group).all()) and int(counts.sum()) == group * G
+    assert bool(((prob.double() - 0.2).abs() <= 2 * R.SUM * 0.2).all())
+    assert abs(float(loss) - 1.0) <= 3 * R.SUM
+
+
+@pytest.mark.parametrize("dtype", R.TYPES)
+@pytest.mark.parametrize("E,rows", [(7, 70_001), (60, 20_001), (300, 1500), (1000, 700)])
+def test_balance_of_groups_in_one_block(E, rows, dtype):
+    """Groups of some hundred rows a lane, a block each, against sums in 64 bits."""
+    G = 513
+    log("one block a group", E, rows, dtype)
+    gen = torch.Generator(device="cuda").manual_seed(367)
+    few = 3  # the groups that are looked at; the others are copies of the last
+    part = torch.randn(few * rows, E, generator=gen, device="cuda").to(dtype)
+    z = torch.cat([part, part[-rows:].repeat(G - few, 1)])
+    choice = torch.randint(0, E, (few * rows, 2), generator=gen, device="cuda", dtype=torch.int32)
+    experts = torch.cat([choice, choice[-rows:].repeat(G - few, 1)])
+    counts, n = torch.zeros(G, E, dtype=torch.int32, device="cuda"), torch.zeros(G, dtype=torch.int32, device="cuda")
+    prob, loss = torch.zeros(G, E, device="cuda"), torch.zeros(1, device="cuda")
+    L.balance_forward(z, experts, None, rows, 1.0, counts, n, prob, loss, L.workspace(G * rows, E, 1))
+    p = torch.softmax(part.double(), 1).reshape(few, rows, E).mean(1)
+    c = torch.stack([torch.bincount(choice[g * rows:(g + 1) * rows].flatten().long(), minlength=E)
+                     for g in range(few)])
+    assert torch.equal(counts[:few].long(), c) and bool((counts[few:] == counts[few - 1]).all())
+    assert bool((n == rows).all())
+    assert bool(((prob[:few].double() - p).abs() <= 2 * R.SUM * p).all())
+    assert torch.equal(prob[few:], prob[few - 1:few].expand(G - few, E))
+    per_group = (E * c.double() / (2 * rows) * p).sum(1)
+    want = float(per_group[:few - 1].sum() + per_group[-1] * (G - few + 1)) / G
+    assert abs(float(loss) - want) <= 3 * R.SUM * want
