@@ -274,8 +274,10 @@ __device__ __forceinline__ float2 sum_below(const SliceView<TYPE, NT> &sl, float
 #pragma unroll 1
     for (uint32_t e0 = 0; e0 < sl.n; e0 += sl.STEP) {
         const Vec<TYPE> v = sl.at(e0);
+        float x[VEC];
 #pragma unroll
-        for (uint32_t e = 0; e < VEC; ++e) sum += v.get(e) < bound ? exp2_fast((v.get(e) - ref) * c) : 0.f;
+        for (uint32_t e = 0; e < VEC; ++e) x[e] = v.get(e) < bound ? exp2_fast((v.get(e) - ref) * c) : 0.f;
+        sum += sum_pairs(x);
     }
     return make_float2(mx, block_sum_f<NT>(sum, red[1]));
 }
@@ -342,7 +344,8 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
             }
         }
 #pragma unroll
-        for (uint32_t e = 0; e < VEC; ++e) sum += to2(x[e]);
+        for (uint32_t e = 0; e < VEC; ++e) x[e] = to2(x[e]);
+        sum += sum_pairs(x);
         asm volatile("" : "+v"(sum));  // now, not when all vectors' numbers are unpacked
     }
     if (lane == 0) sh.listed[w] = listed;

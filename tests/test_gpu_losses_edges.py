@@ -260,3 +260,29 @@ def test_balance_of_groups_in_one_block(E, rows, dtype):
     per_group = (E * c.double() / (2 * rows) * p).sum(1)
     want = float(per_group[:few - 1].sum() + per_group[-1] * (G - few + 1)) / G
     assert abs(float(loss) - want) <= 3 * R.SUM * want
+
+
+@pytest.mark.parametrize("dtype", R.TYPES)
+def test_distill_of_the_longest_rows_of_one_block(dtype):
+    """Rows of 2^18 columns, whose threads add more numbers one after the other than any: equal ones, which all round
+    the same way, and others."""
+    cols, rows, k = 1 << 18, 128, 20
+    log("2^18 columns", dtype)
+    z, idx, val, rest = R.student(rows, cols, k, dtype, 373)
+    z[0] = 0.3
+    z[1] = torch.where(torch.arange(cols) % 3 == 0, 0.7, -0.4).to(dtype)
+    weight = torch.zeros(rows)
+    weight[:4] = 1.0
+    check_step(z, idx, val, rest, 1.0, 40.0, weight)
+
+
+@pytest.mark.parametrize("dtype", R.TYPES)
+def test_top_rest_of_equal_numbers(dtype):
+    """Slices of sixteen vectors a thread whose exponentials all round the same way."""
+    for cols in (65_536, 131_072):
+        log("equal numbers", cols, dtype)
+        x = torch.full((3, cols), -1.3)
+        x[:, :100] = torch.linspace(0.0, 5.0, 100)
+        x[1, 200:] = torch.where(torch.arange(cols - 200) % 5 == 0, -0.7, -2.1)
+        x[2, 1000:] += torch.arange(cols - 1000) * -1e-5
+        check_top(x.to(dtype).cuda(), 64)
