@@ -64,14 +64,16 @@ __device__ __forceinline__ float2 slice_again(const typename Num<TYPE>::T *p, ui
         for (uint32_t e0 = threadIdx.x * VEC; e0 < n; e0 += STEP) {
             const Vec<TYPE> v = load_vec<TYPE, false>(p, e0, n, avail);
             const uint32_t b = kept_bits<VEC>(bm, e0 / VEC);
+            float x[VEC];
 #pragma unroll
             for (uint32_t e = 0; e < VEC; ++e) {
-                const float x = b >> e & 1u ? F_NEG_INF : v.get(e);
+                x[e] = b >> e & 1u ? F_NEG_INF : v.get(e);
                 if (pass == 0)
-                    mx = fmaxf(mx, x);
+                    mx = fmaxf(mx, x[e]);
                 else
-                    sum += exp2_fast((x - ref) * c);
+                    x[e] = exp2_fast((x[e] - ref) * c);
             }
+            if (pass != 0) sum += sum_pairs(x);
         }
         if (pass == 0)
             mx = block_max_f<THREADS>(mx, red[0]);
@@ -117,8 +119,10 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_slice(DistillArgs a) {
     for (int i = 0; i < NV; ++i) {
         if (i * DIST_THREADS * VEC >= n) break;
         v[i].keep_packed();
+        float x[VEC];
 #pragma unroll
-        for (uint32_t e = 0; e < VEC; ++e) sum += to2(v[i].get(e));
+        for (uint32_t e = 0; e < VEC; ++e) x[e] = to2(v[i].get(e));
+        sum += sum_pairs(x);
         asm volatile("" : "+v"(sum));  // one vector's numbers after the other
     }
     sum = block_sum_f<DIST_THREADS>(sum, red[1]);
@@ -364,8 +368,10 @@ __device__ __forceinline__ float sum_run(Vec<TYPE> (&v)[NV], uint32_t n, uint32_
         if (b) v[i].mask(b);
         v[i].keep_packed();
         if (MAX) most.add(v[i]);
+        float x[VEC];
 #pragma unroll
-        for (uint32_t e = 0; e < VEC; ++e) sum += to2(v[i].get(e));
+        for (uint32_t e = 0; e < VEC; ++e) x[e] = to2(v[i].get(e));
+        sum += sum_pairs(x);
         asm volatile("" : "+v"(sum));  // one vector's numbers after the other
     }
     return sum;
@@ -576,6 +582,9 @@ static_assert(!forward_by_rows(1u << 30, TYPE_F32) && !forward_by_rows((1u << 30
                   !forward_by_rows(1u << 30, TYPE_BF16) && !forward_by_rows(0x7fffffffu, TYPE_F16) &&
                   forward_by_rows(8192, TYPE_F32) && !forward_by_rows(16385, TYPE_F16),
               "rows by their bytes, also where these pass 32 bits");
+
+// A thread of a row's block adds one sum a vector, of 64 vectors at most.
+static_assert(ROW_MAX_COLS <= 64 * 1024 * Num<TYPE_F32>::VEC && 16384 <= 64 * 256 * Num<TYPE_BF16>::VEC, "longest sums");
 
 // Threads per row: as many as hold it in RES vectors each, but 512 up to twice
 // that, where three blocks share a CU and one of 1024 threads would have it for
