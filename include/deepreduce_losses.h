@@ -74,8 +74,9 @@ typedef struct {
     uint32_t val_type;   /* DR_TYPE_* */
 } dr_teacher;
 
-/* Scratch bytes sufficient for any call below on a matrix of rows x cols
- * numbers with k kept logits (0 for an argument out of its range). */
+/* Scratch bytes sufficient for any call below on a matrix of at most rows x
+ * cols numbers with at most k kept logits (0 for an argument out of its
+ * range). */
 DR_EXPORT size_t dr_losses_workspace_bytes(uint64_t rows, uint64_t cols, uint32_t k);
 
 /* ---------------------------------------------------------------------- */

@@ -513,8 +513,9 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 || !GRAD ? 8 : 6) void k_dis
     }
 }
 
+constexpr uint64_t SLICES = 512;  // that a call is to have, if shorter ones make them
 Slices distill_slices(const Matrix &m) {
-    return plan_slices(m.rows, m.cols, 16 / type_bytes(m.type), DIST_THREADS, DIST_NV, 512);
+    return plan_slices(m.rows, m.cols, 16 / type_bytes(m.type), DIST_THREADS, DIST_NV, SLICES);
 }
 
 DistillArgs distill_args(const Matrix &m, const Teacher &t, float temperature, const float *weight) {
@@ -644,9 +645,13 @@ uint64_t distill_threads(const Matrix &m) {
     return m.rows * std::max<uint64_t>(row_threads(m), (uint64_t)distill_slices(m).n * DIST_THREADS);
 }
 
+// For as many rows and columns or fewer: fewer rows are cut into more slices
+// each, down to 512 in all, so that there are the longest slices of all rows,
+// or less than twice 512.
 size_t distill_ws_bytes(uint64_t rows, uint64_t cols, uint32_t type) {
-    const Matrix m = {nullptr, rows, cols, (uint32_t)cols, type};
-    return part_bytes(m) + rows * STATS * sizeof(float);
+    const uint64_t longest = (uint64_t)DIST_THREADS * DIST_NV * (16 / type_bytes(type));
+    const uint64_t slices = std::max<uint64_t>(rows * ((cols + longest - 1) / longest), 2 * SLICES);
+    return slices * sizeof(float2) + 256 + rows * STATS * sizeof(float);
 }
 
 hipError_t launch_distill_forward(const Matrix &m, const Teacher &t, float temperature, const float *weight,

@@ -118,10 +118,10 @@ size_t dr_losses_workspace_bytes(uint64_t rows, uint64_t cols, uint32_t k) {
     }
     size_t n = 256;
     for (uint32_t type : {TYPE_F32, TYPE_BF16}) {
-        if (k >= 1 && k <= DR_MAX_TOP) n = std::max(n, plan_top(rows, cols, k, type).bytes);
+        if (k >= 1) n = std::max(n, plan_top(rows, cols, std::min(k, DR_MAX_TOP), type).bytes);
         n = std::max(n, distill_ws_bytes(rows, cols, type));
     }
-    if (cols <= DR_MAX_EXPERTS) n = std::max(n, balance_ws_bytes(rows, cols));
+    n = std::max(n, balance_ws_bytes(rows, std::min<uint64_t>(cols, DR_MAX_EXPERTS)));
     return align_up(n, 256);
 }
 

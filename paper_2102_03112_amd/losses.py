@@ -168,7 +168,7 @@ def _check(fn: str, status: int):
 
 
 def workspace_bytes(rows: int, cols: int, k: int = 1) -> int:
-    """Scratch bytes for any call below on rows x cols logits with k kept ones."""
+    """Scratch bytes for any call below on at most rows x cols logits with at most k kept ones."""
     n = int(lib().dr_losses_workspace_bytes(rows, cols, k))
     if n == 0:
         raise DeepReduceError("dr_losses_workspace_bytes", DR_EINVAL, last_error())

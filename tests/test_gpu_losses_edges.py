@@ -286,3 +286,21 @@ def test_top_rest_of_equal_numbers(dtype):
         x[1, 200:] = torch.where(torch.arange(cols - 200) % 5 == 0, -0.7, -2.1)
         x[2, 1000:] += torch.arange(cols - 1000) * -1e-5
         check_top(x.to(dtype).cuda(), 64)
+
+
+@pytest.mark.parametrize("dtype", R.TYPES)
+def test_a_workspace_of_the_longest_batch_serves_shorter_ones(dtype):
+    rows, cols, k = 512, 40_000, 20
+    z, idx, val, rest = (x.cuda() for x in R.student(8, cols, k, dtype, 379))
+    ws = L.workspace(rows, cols, k)
+    many = [x.repeat(rows // 8, *[1] * (x.dim() - 1)) for x in (z, idx, val, rest)]
+    seen = {}
+    for n in (512, 511, 300, 100, 8, 1):
+        zn, teacher = many[0][:n], L.Teacher(*(x[:n] for x in many[1:]))
+        loss, stats, loss2 = torch.zeros(n, device="cuda"), torch.zeros(n, L.STATS, device="cuda"), torch.zeros(n, device="cuda")
+        grad = torch.zeros_like(zn)
+        L.distill_forward(zn, teacher, 1.0, None, loss, stats, ws)
+        L.distill_step(zn, teacher, 1.0, None, loss2, grad, ws)
+        seen[n] = loss[0].item(), loss2[0].item()
+    want = float(R.distill(z[:1].cpu(), idx.cpu(), val.cpu(), rest.cpu(), 1.0)[0])
+    assert all(abs(x - want) <= 2 * R.SUM + 2.0 ** -22 * 40 for pair in seen.values() for x in pair)

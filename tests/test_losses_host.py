@@ -169,6 +169,24 @@ def test_workspace_bytes(lib):
     assert f(131_072, 256, 8) < 16 << 20
 
 
+def test_a_workspace_serves_smaller_calls(lib):
+    """Bytes never fall as rows, columns or kept logits grow: what serves a batch serves a shorter one."""
+    f = lib.dr_losses_workspace_bytes
+    rows = list(range(1, 70)) + [100, 127, 128, 129, 255, 256, 257, 300, 511, 512, 513, 1000, 1023, 1024, 1025, 4096]
+    cols = [1, 8, 300, 1024, 1025, 2000, 8192, 16384, 16385, 32000, 40_000, 65536, 65537, 131_072, 1 << 20]
+    for k in (0, 1, 64, 256, 257, 1024):
+        for c in cols:
+            need = [f(r, c, k) for r in rows]
+            assert need == sorted(need), (c, k)
+        for r in rows[::9]:
+            need = [f(r, c, k) for c in cols]
+            assert need == sorted(need), (r, k)
+    for r in rows[::9]:
+        for c in cols:
+            need = [f(r, c, k) for k in (0, 1, 2, 8, 50, 64, 200, 256, 257, 1024)]
+            assert need == sorted(need), (r, c)
+
+
 def test_python_checks():
     z = torch.zeros(4, 10)
     with pytest.raises(ValueError):  # not on a GPU
