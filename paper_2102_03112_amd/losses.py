@@ -169,6 +169,7 @@ def _check(fn: str, status: int):
 
 def workspace_bytes(rows: int, cols: int, k: int = 1) -> int:
     """Scratch bytes for any call below on at most rows x cols logits with at most k kept ones."""
+    _need(0 <= rows < 1 << 64 and 0 <= cols < 1 << 64 and 0 <= k < 1 << 32, "rows, cols or k out of range")
     n = int(lib().dr_losses_workspace_bytes(rows, cols, k))
     if n == 0:
         raise DeepReduceError("dr_losses_workspace_bytes", DR_EINVAL, last_error())
@@ -191,6 +192,7 @@ def workspace(rows: int, cols: int, k: int = 1, device="cuda"):
 def top_logits(logits, k: int, temperature: float, idx_out, val_out, rest_out, ws, stream=None):
     """The k largest logits of each row and the entry for the rest (dr_top_logits)."""
     m, rows, _, dev = _logits(logits)
+    _need(0 <= k < 1 << 32, "k out of range")
     _check("dr_top_logits", lib().dr_top_logits(
         ctypes.byref(m), k, temperature, _flat(idx_out, rows * k, _I32, dev, "idx_out"),
         _flat(val_out, rows * k, _F32, dev, "val_out"), _flat(rest_out, rows, _F32, dev, "rest_out"),
@@ -270,7 +272,8 @@ def _mask(mask, rows: int, dev: int):
 
 
 def _groups(rows: int, group_rows: int) -> int:
-    _need(group_rows >= 1, "group_rows must be at least 1")
+    # cut to 64 bits, it would have more groups than the outputs are checked for here
+    _need(1 <= group_rows < 1 << 64, "group_rows out of range")
     return -(-rows // group_rows)
 
 
@@ -297,6 +300,7 @@ def balance_backward(logits, k: int, row_mask, group_rows: int, coef: float, cou
     rows_in then) or the sums over all workers; upstream: one float32, or None for 1."""
     m, rows, E, dev = _logits(logits)
     G = _groups(rows, group_rows)
+    _need(0 <= k < 1 << 32, "k out of range")
     r = DrRoutes(None, 0, k, INDEX_I32, _mask(row_mask, rows, dev), group_rows)
     _check("dr_balance_backward", lib().dr_balance_backward(
         ctypes.byref(m), ctypes.byref(r), coef, _flat(counts, G * E, _I32, dev, "counts"),

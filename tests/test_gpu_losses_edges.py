@@ -304,3 +304,20 @@ def test_a_workspace_of_the_longest_batch_serves_shorter_ones(dtype):
         seen[n] = loss[0].item(), loss2[0].item()
     want = float(R.distill(z[:1].cpu(), idx.cpu(), val.cpu(), rest.cpu(), 1.0)[0])
     assert all(abs(x - want) <= 2 * R.SUM + 2.0 ** -22 * 40 for pair in seen.values() for x in pair)
+
+
+def test_numbers_that_a_c_integer_would_cut_are_refused():
+    z = torch.zeros(6, 8, device="cuda")
+    e = torch.zeros(6, 2, dtype=torch.int32, device="cuda")
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")  # noqa: E731
+    loss, ws = torch.zeros(1, device="cuda"), L.workspace(6, 8, 2)
+    for group in (0, -1, (1 << 64) + 3):
+        with pytest.raises(ValueError):
+            L.balance_forward(z, e, None, group, 1.0, i32(1, 8), i32(1), None, loss, ws)
+        with pytest.raises(ValueError):
+            L.balance_backward(z, 2, None, group, 1.0, i32(1, 8), i32(1), i32(1), None, z)
+    for k in (-1, (1 << 32) + 2):
+        with pytest.raises(ValueError):
+            L.balance_backward(z, k, None, 6, 1.0, i32(1, 8), i32(1), i32(1), None, z)
+        with pytest.raises(ValueError):
+            L.top_logits(z, k, 1.0, None, None, None, ws)

@@ -224,3 +224,16 @@ def test_the_definitions_gradients_against_differences():
         down[r, j] -= h
         d = (R.balance(up, experts, 2, None, 7, 0.3)[3] - R.balance(down, experts, 2, None, 7, 0.3)[3]) / (2 * h)
         assert abs(d - float(grad[r, j])) < 1e-9
+
+
+@pytest.mark.parametrize("bad", [-1, 1 << 64, (1 << 64) + 5])
+def test_python_refuses_numbers_that_a_c_integer_would_cut(bad):
+    """Before the call: a number of group rows cut to 64 bits would have more groups than the outputs are checked for."""
+    with pytest.raises(ValueError):
+        L._groups(10, bad)
+    with pytest.raises(ValueError):
+        L.workspace_bytes(bad, 10)
+    with pytest.raises(ValueError):
+        L.workspace_bytes(10, bad)
+    with pytest.raises(ValueError):
+        L.workspace_bytes(10, 10, bad)
