@@ -87,9 +87,10 @@ DR_EXPORT size_t dr_losses_workspace_bytes(uint64_t rows, uint64_t cols, uint32_
  * columns and values of the k largest logits, by value descending, of equal
  * values the lowest column first.  -inf is never kept: places left over hold
  * column -1 and value -inf.  rest_out (nullable, one per row) receives ln of
- * the sum of exp(logit / temperature) over the columns not kept, -inf if that
- * sum is 0.  EINVAL: k outside 1 .. DR_MAX_TOP, temperature not finite or not
- * above 0, a null pointer, workspace too small. */
+ * the sum of exp(logit / temperature) over the columns not kept (a float's
+ * largest or lowest where that is beyond it), -inf if that sum is 0.  EINVAL:
+ * k outside 1 .. DR_MAX_TOP, temperature not finite or not above 0, a null
+ * pointer, workspace too small. */
 DR_EXPORT dr_status dr_top_logits(const dr_logits *logits_h, uint32_t k, float temperature, int32_t *idx_out,
                                   float *val_out, float *rest_out, void *ws, size_t ws_bytes, void *stream);
 

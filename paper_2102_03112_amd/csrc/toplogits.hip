@@ -167,8 +167,11 @@ __device__ __forceinline__ void top_finish(const TopArgs &a, uint64_t row, uint6
         a.idx_out[row * K + i] = i < n ? (int32_t)(0xffffffffu - (uint32_t)key) : -1;
         a.val_out[row * K + i] = i < n ? key_value(key) : F_NEG_INF;
     }
-    if (threadIdx.x == 0 && a.rest_out)
-        a.rest_out[row] = sum > 0.f ? (float)((double)ref * (double)a.inv_t + ln_sum(sum)) : F_NEG_INF;
+    // finite where anything is left, also beyond a float's range: -inf would say that nothing is
+    if (threadIdx.x == 0 && a.rest_out) {
+        const double rest = (double)ref * (double)a.inv_t + ln_sum(sum);
+        a.rest_out[row] = sum > 0.f ? (float)fmin(fmax(rest, (double)F_LOWEST), -(double)F_LOWEST) : F_NEG_INF;
+    }
 }
 
 // A slice as the rare paths read it: again from memory, one vector per thread

@@ -321,3 +321,23 @@ def test_numbers_that_a_c_integer_would_cut_are_refused():
             L.balance_backward(z, k, None, 6, 1.0, i32(1, 8), i32(1), i32(1), None, z)
         with pytest.raises(ValueError):
             L.top_logits(z, k, 1.0, None, None, None, ws)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [50, 9000, 70_001])
+def test_top_rest_beyond_a_floats_range(cols, dtype):
+    """Rows masked with the lowest number, over a temperature below 1: the rest is as low as a float goes, and not the
+    -inf that says that nothing is left; a student of such a payload has a finite loss and gradient."""
+    log("rest beyond", cols, dtype)
+    low, top = torch.finfo(dtype).min, torch.finfo(dtype).max
+    gen = torch.Generator().manual_seed(383)
+    x = torch.randn(4, cols, generator=gen)
+    x[0], x[1], x[2, 8:] = low, top, -math.inf
+    x = x.to(dtype).cuda()
+    idx, val, rest = run_top(x, 8, 0.7)
+    f32 = torch.finfo(F32)
+    assert rest.tolist()[:3] == [f32.min, f32.max, -math.inf] and abs(float(rest[3])) < 100.0
+    z = torch.randn(4, cols, generator=gen).to(dtype).cuda()
+    keep = torch.tensor([0, 2, 3])
+    for out in run_distill(z[keep], idx.cpu()[keep], val.cpu()[keep], rest.cpu()[keep], 0.7, None):
+        assert bool(torch.isfinite(out).all())
