@@ -142,6 +142,7 @@ __device__ __forceinline__ float rescale(float x, float a, float b, float c) {
 // teacher's y, or tells that there is none.  All lanes of a wave take part.
 struct RowResult {
     double loss;  // not yet times the weight
+    double a_tail;  // stats[3] in 64 bits
     float stats[6];
 };
 template <typename ENTRY>
@@ -201,6 +202,7 @@ __device__ __forceinline__ RowResult row_result(float m_tail, double tail, uint3
     r.stats[1] = sum_q > 0.0 ? (float)(1.0 / sum_q) : 0.f;
     r.stats[2] = m_tail;
     r.stats[3] = (float)a_tail;
+    r.a_tail = a_tail;
     r.stats[4] = m_p;
     r.stats[5] = sum_p > 0.0 ? (float)(1.0 / sum_p) : 0.f;
     return r;
@@ -456,11 +458,14 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 || !GRAD ? 8 : 6) void k_dis
         ref = mx > F_NEG_INF ? mx : ref;
     }
     float tail = sum * by_top.to(ref);
-    if (!(sum > 1e-28f && sum < 1e30f && tail > 1e-30f && tail < 1e30f)) {
+    // where nearly all lies far below the reference, numbers that count would be below a float's range
+    if (!(sum > 1e-26f && sum < 1e30f && tail > 1e-30f && tail < 1e30f)) {
         const float2 x = slice_again<TYPE, THREADS>(p, n, avail, bm, a.c, red + 2);
         ref = x.x;
         tail = x.y;
     }
+    // the tail's power of two: a step's gradients are relative to it, so that they have a float's whole range
+    const int size = GRAD && tail > 0.f ? __builtin_amdgcn_frexp_expf(tail) : 0;
     if (threadIdx.x < 64) {
         const auto entry = [&](uint32_t i, float &student, float &teacher) {
             const uint32_t k = i * 64 + threadIdx.x;
@@ -477,7 +482,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 || !GRAD ? 8 : 6) void k_dis
 #pragma unroll
             for (uint32_t i = 0; i < 6; ++i) st = threadIdx.x == i ? r.stats[i] : st;
             if (!GRAD && threadIdx.x < STATS) a.stats[row * STATS + threadIdx.x] = st;
-            if (GRAD && threadIdx.x < 6) row_stats[threadIdx.x] = st;
+            if (GRAD && threadIdx.x < 6) row_stats[threadIdx.x] = threadIdx.x == 3 ? (float)ldexp(r.a_tail, size) : st;
         }
     }
     if constexpr (!GRAD) return;
@@ -485,15 +490,18 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 || !GRAD ? 8 : 6) void k_dis
     const float m = row_stats[0] == F_NEG_INF ? 0.f : row_stats[0], scale = w * a.inv_t;
     const float q = row_stats[5] > 0.f ? scale * row_stats[1] : 0.f;  // no gradient without a teacher's distribution
     ref = ref == F_NEG_INF ? 0.f : ref;
-    const Base2 to2(ref, a.c);
-    const float f = scale * row_stats[3], f2 = f * to2.to(ref);
+    // f 2^(z c - R) with R larger by `size` and f, too, as far as R's rounding lets it
+    Base2 to2(ref, a.c);
+    const float r = to2.r, f = scale * row_stats[3];
+    to2.r += (float)size;
+    const float f2 = ldexpf(f * Base2(ref, a.c).to(ref), (int)(to2.r - r) - size);
     if (fabsf(ref * a.c) >= 1e30f) {  // all near the lowest number
 #pragma unroll 1
         for (uint32_t e0 = threadIdx.x * VEC; e0 < n; e0 += STEP) {
             const Vec<TYPE> u = load_vec<TYPE, false>(p, e0, n, avail);
             float x[VEC];
 #pragma unroll
-            for (uint32_t e = 0; e < VEC; ++e) x[e] = f * exp2_fast((u.get(e) - ref) * a.c);
+            for (uint32_t e = 0; e < VEC; ++e) x[e] = f * exp2_fast((u.get(e) - ref) * a.c - (float)size);
             store_vec<TYPE>(out, e0, n, x);
         }
     } else {

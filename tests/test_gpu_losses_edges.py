@@ -341,3 +341,17 @@ def test_top_rest_beyond_a_floats_range(cols, dtype):
     keep = torch.tensor([0, 2, 3])
     for out in run_distill(z[keep], idx.cpu()[keep], val.cpu()[keep], rest.cpu()[keep], 0.7, None):
         assert bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [900, 5000, 30_000])
+@pytest.mark.parametrize("gap,weight", [(30.0, 1.0), (45.0, 1.0), (55.0, 1.0), (-50.0, 1e-9), (-65.0, 1e-9)])
+def test_distill_gradients_of_a_tail_far_from_the_kept_logits(cols, gap, weight, dtype):
+    """The small gradients of a tail that lies far below the kept logits, or far above them, are as exact as others."""
+    log("far tail", cols, gap, dtype)
+    z, idx, val, rest = R.student(130, cols, 8, dtype, 389, spread=6.0)
+    kept = torch.zeros(130, cols, dtype=torch.bool).scatter_(1, idx.long(), True)
+    z = torch.where(kept, z.float() + gap, z.float()).to(dtype)
+    w = torch.zeros(130)
+    w[:4] = weight
+    check_step(z, idx, val, rest, 1.0, 130.0, w)
