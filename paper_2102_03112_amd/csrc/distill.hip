@@ -73,7 +73,7 @@ __device__ __forceinline__ float2 slice_again(const typename Num<TYPE>::T *p, ui
                 else
                     x[e] = exp2_fast((x[e] - ref) * c);
             }
-            if (pass != 0) sum += sum_pairs(x);
+            if (pass != 0) add_fours(sum, x);
         }
         if (pass == 0)
             mx = block_max_f<THREADS>(mx, red[0]);
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_slice(DistillArgs a) {
         float x[VEC];
 #pragma unroll
         for (uint32_t e = 0; e < VEC; ++e) x[e] = to2(v[i].get(e));
-        sum += sum_pairs(x);
+        add_fours(sum, x);
         asm volatile("" : "+v"(sum));  // one vector's numbers after the other
     }
     sum = block_sum_f<DIST_THREADS>(sum, red[1]);
@@ -139,15 +139,15 @@ __device__ __forceinline__ float rescale(float x, float a, float b, float c) {
 // A row's result from its columns not kept (m_tail, tail: a reference at least
 // near their maximum, and their sum relative to it) and its kept entries:
 // entry(i, x, y) gives the lane's i-th of n, the student's logit x and the
-// teacher's y, or tells that there is none.  All lanes of a wave take part.
+// teacher's y, or tells that there is none.  stats[3] is times 2^size.  All
+// lanes of a wave take part.
 struct RowResult {
     double loss;  // not yet times the weight
-    double a_tail;  // stats[3] in 64 bits
     float stats[6];
 };
 template <typename ENTRY>
 __device__ __forceinline__ RowResult row_result(float m_tail, double tail, uint32_t n, ENTRY entry, float rest, float c,
-                                                float inv_t) {
+                                                float inv_t, int size = 0) {
     float y0 = F_NEG_INF, m = m_tail, x, y;
 #pragma unroll
     for (uint32_t i = 0; i < n; ++i)
@@ -157,9 +157,6 @@ __device__ __forceinline__ RowResult row_result(float m_tail, double tail, uint3
         }
     m = wave_max_f(m);
     y0 = wave_max_f(y0);
-    // The teacher's reference: the largest logit over the temperature, or rest.
-    const double y0_t = y0 == F_NEG_INF ? (double)y0 : fmin(fmax((double)y0 * inv_t, (double)F_LOWEST), -(double)F_LOWEST);
-    const float m_p = fmaxf((float)y0_t, rest);
     // Sums relative to y0 and m; d: the entry's ln of p over q but for the
     // sums.  Logits are taken off one another before anything else, so that
     // large ones, a mask's lowest number say, leave no error of their size.
@@ -178,6 +175,9 @@ __device__ __forceinline__ RowResult row_result(float m_tail, double tail, uint3
     sum_q = wave_sum_f64(sum_q) + tail_q;
     sum_p = wave_sum_f64(sum_p);
     sum_d = wave_sum_f64(sum_d);
+    // The teacher's reference: the largest logit over the temperature, or rest.
+    const double y0_t = y0 == F_NEG_INF ? (double)y0 : fmin(fmax((double)y0 * inv_t, (double)F_LOWEST), -(double)F_LOWEST);
+    const float m_p = fmaxf((float)y0_t, rest);
     const float y0_p = y0 == F_NEG_INF ? 0.f : exp_below((float)(y0_t - m_p));  // and now relative to m_p
     sum_d = y0_p > 0.f ? y0_p * (sum_d + (y0_t - m_p) * sum_p) : 0.0;
     sum_p *= y0_p;
@@ -201,8 +201,7 @@ __device__ __forceinline__ RowResult row_result(float m_tail, double tail, uint3
     r.stats[0] = m;
     r.stats[1] = sum_q > 0.0 ? (float)(1.0 / sum_q) : 0.f;
     r.stats[2] = m_tail;
-    r.stats[3] = (float)a_tail;
-    r.a_tail = a_tail;
+    r.stats[3] = (float)ldexp(a_tail, size);
     r.stats[4] = m_p;
     r.stats[5] = sum_p > 0.0 ? (float)(1.0 / sum_p) : 0.f;
     return r;
@@ -373,7 +372,7 @@ __device__ __forceinline__ float sum_run(Vec<TYPE> (&v)[NV], uint32_t n, uint32_
         float x[VEC];
 #pragma unroll
         for (uint32_t e = 0; e < VEC; ++e) x[e] = to2(v[i].get(e));
-        sum += sum_pairs(x);
+        add_fours(sum, x);
         asm volatile("" : "+v"(sum));  // one vector's numbers after the other
     }
     return sum;
@@ -400,7 +399,7 @@ __device__ __forceinline__ void grad_run(Vec<TYPE> (&v)[NV], typename Num<TYPE>:
 }
 
 template <uint32_t TYPE, uint32_t THREADS, bool GRAD>
-__global__ __launch_bounds__(THREADS, THREADS < 512 || !GRAD ? 8 : 6) void k_distill_row(DistillArgs a) {
+__global__ __launch_bounds__(THREADS, !GRAD ? 8 : THREADS < 512 ? 7 : 6) void k_distill_row(DistillArgs a) {
     using N = Num<TYPE>;
     using T = typename N::T;
     constexpr uint32_t VEC = N::VEC, STEP = THREADS * VEC, CHUNK = RES * STEP;
@@ -475,14 +474,14 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 || !GRAD ? 8 : 6) void k_dis
             return true;
         };
         const RowResult r = row_result(ref, tail, (a.t.k + 63) / 64, entry, a.t.rest ? a.t.rest[row] : F_NEG_INF, a.c,
-                                       a.inv_t);
+                                       a.inv_t, size);
         if (threadIdx.x == 0) a.loss[row] = (float)(w * r.loss);
         if (GRAD || a.stats) {
             float st = 0.f;
 #pragma unroll
             for (uint32_t i = 0; i < 6; ++i) st = threadIdx.x == i ? r.stats[i] : st;
             if (!GRAD && threadIdx.x < STATS) a.stats[row * STATS + threadIdx.x] = st;
-            if (GRAD && threadIdx.x < 6) row_stats[threadIdx.x] = threadIdx.x == 3 ? (float)ldexp(r.a_tail, size) : st;
+            if (GRAD && threadIdx.x < 6) row_stats[threadIdx.x] = st;
         }
     }
     if constexpr (!GRAD) return;
@@ -592,8 +591,8 @@ static_assert(!forward_by_rows(1u << 30, TYPE_F32) && !forward_by_rows((1u << 30
                   forward_by_rows(8192, TYPE_F32) && !forward_by_rows(16385, TYPE_F16),
               "rows by their bytes, also where these pass 32 bits");
 
-// A thread of a row's block adds one sum a vector, of 64 vectors at most.
-static_assert(ROW_MAX_COLS <= 64 * 1024 * Num<TYPE_F32>::VEC && 16384 <= 64 * 256 * Num<TYPE_BF16>::VEC, "longest sums");
+// A thread of a row's block adds a number for four of the row's, 64 at most.
+static_assert(ROW_MAX_COLS <= 64 * 1024 * 4 && 16384 <= 64 * 256 * 4, "longest sums");
 
 // Threads per row: as many as hold it in RES vectors each, but 512 up to twice
 // that, where three blocks share a CU and one of 1024 threads would have it for

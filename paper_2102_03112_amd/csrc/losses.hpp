@@ -347,14 +347,13 @@ struct Base2 {
 };
 __device__ __forceinline__ bool sum_in_range(float s) { return s > 0.25f && s < 1e30f; }
 
-// The sum of a vector's numbers by pairs: as many additions as one after the
-// other, and roundings of three (fp32: two) on the way.  A thread's own sum is
-// then a chain of one addition for a vector: of 64 vectors at most.
+// Adds a vector's numbers by fours, in pairs: as many additions as one after
+// the other, of which a thread's sum meets one for four numbers, so that it is
+// a chain of 64 at most.
 template <uint32_t N>
-__device__ __forceinline__ float sum_pairs(const float (&x)[N]) {
-    float s = (x[0] + x[1]) + (x[2] + x[3]);
-    if constexpr (N == 8) s += (x[4] + x[5]) + (x[6] + x[7]);
-    return s;
+__device__ __forceinline__ void add_fours(float &sum, const float (&x)[N]) {
+#pragma unroll
+    for (uint32_t i = 0; i < N; i += 4) sum += (x[i] + x[i + 1]) + (x[i + 2] + x[i + 3]);
 }
 
 // ln of a sum: the exponent apart, so that the logarithm's own error (of a

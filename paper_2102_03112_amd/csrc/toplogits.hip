@@ -280,7 +280,7 @@ __device__ __forceinline__ float2 sum_below(const SliceView<TYPE, NT> &sl, float
         float x[VEC];
 #pragma unroll
         for (uint32_t e = 0; e < VEC; ++e) x[e] = v.get(e) < bound ? exp2_fast((v.get(e) - ref) * c) : 0.f;
-        sum += sum_pairs(x);
+        add_fours(sum, x);
     }
     return make_float2(mx, block_sum_f<NT>(sum, red[1]));
 }
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
         }
 #pragma unroll
         for (uint32_t e = 0; e < VEC; ++e) x[e] = to2(x[e]);
-        sum += sum_pairs(x);
+        add_fours(sum, x);
         asm volatile("" : "+v"(sum));  // now, not when all vectors' numbers are unpacked
     }
     if (lane == 0) sh.listed[w] = listed;
