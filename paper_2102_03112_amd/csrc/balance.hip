@@ -27,7 +27,7 @@ struct BalanceArgs {
     uint32_t *prows;
     uint32_t col_blocks;  // joining blocks per group
     double *gloss;        // sum_e f P per group, or per joining block
-    uint32_t *done;       // not null: the joining blocks that have left theirs
+    unsigned long long *total;  // not null: the sum of all joining blocks' and their number
     int32_t *counts_out, *rows_out;
     float *prob_out, *loss_out;
     // backward
@@ -147,7 +147,10 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
     const Rows b = block_rows(a);
     for (uint32_t e = threadIdx.x; e < E; e += BT) hist[e] = 0;
     if (threadIdx.x == 0) rows = 0;
-    if (blockIdx.x == 0 && threadIdx.x == 0 && a.done) *a.done = 0;
+    if (blockIdx.x == 0 && a.total) {  // of the launch after this one
+        if (threadIdx.x == 0) *a.total = 0;
+        if (threadIdx.x < a.r.groups * a.col_blocks) a.gloss[threadIdx.x] = 0.0;
+    }
     float acc[N] = {};
     uint32_t n = 0, added = 0;
     bool folded = false;
@@ -229,27 +232,48 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
 constexpr uint32_t JOIN_COLS = 16, ONE_JOIN_COLS = 64;
 
 // The loss from those of up to MAX_ADDING joining blocks, without a launch for
-// it: each leaves its own and then counts itself, and the last one that does
-// adds them, in 64 bits and in their order.  All of it by atomic operations,
-// which take place where every block sees them; one that returns is done, and
-// so the count's operand is made from what leaving the loss returned.  Each
-// operation on the one count takes some 10 ns, so that more blocks leave their
-// losses to a launch.
-constexpr uint32_t MAX_ADDING = 64;
+// it: added as whole numbers of 2^-LOSS_BITS, whose order cannot show, above two
+// counts, of the blocks and of those that left their loss in a place of its
+// own instead; one atomic operation adds a block's loss and tells the last block
+// that it is.  A loss from 2^-13 on is then rounded by 2^-27 of itself at most;
+// a smaller one, or one that is NaN, is left, in 64 bits, and the last block adds
+// what was left in the blocks' order.  (Blocks of 16 experts: 64 blocks' groups
+// times experts are 2^10 at most, and so is the sum of all f P, which takes 50
+// bits.)  Leaving is an atomic operation, too, so that it takes place where
+// every block sees it; it is done when it returns, and the count's operand is
+// made from what it returned.  Each operation on the one word takes some 10 ns,
+// so that more blocks leave their losses to a launch (131072 x 256: 16 blocks 4
+// us less than with that launch, 512 blocks 5 us more).
+constexpr uint32_t MAX_ADDING = 64, LOSS_BITS = 39, COUNT_BITS = 7;
 __device__ __forceinline__ void add_losses(const BalanceArgs &a, double loss) {  // the first wave; loss: lane 0's
+    constexpr double ONE = (double)(1ull << LOSS_BITS), SMALL = 1.0 / 8192;
+    constexpr unsigned long long COUNT = (1ull << COUNT_BITS) - 1;
     auto *const left = (unsigned long long *)a.gloss;
     const uint32_t lane = threadIdx.x;
-    uint32_t last = 0;
+    unsigned long long sum = 0;
+    uint32_t last = 0;  // 1: this block is the last one, 2: and others left their loss
     if (lane == 0) {
-        const unsigned long long was = atomicExch(&left[blockIdx.x], __builtin_bit_cast(unsigned long long, loss));
-        uint32_t one;
-        asm volatile("v_mov_b32 %0, 1" : "=v"(one) : "v"((uint32_t)was));
-        last = atomicAdd(a.done, one) + 1 == gridDim.x ? 1u : 0u;
+        unsigned long long add = 1;
+        if (loss >= SMALL) {
+            add |= (unsigned long long)(loss * ONE + 0.5) << 2 * COUNT_BITS;
+        } else if (loss != 0.0) {
+            const unsigned long long was = atomicExch(&left[blockIdx.x], __builtin_bit_cast(unsigned long long, loss));
+            uint32_t one;
+            asm volatile("v_mov_b32 %0, 1" : "=v"(one) : "v"((uint32_t)was));
+            add = one << COUNT_BITS | one;
+        }
+        sum = atomicAdd(a.total, add) + add;
+        if ((sum & COUNT) == gridDim.x) last = sum >> COUNT_BITS & COUNT ? 2 : 1;
     }
-    if (!__builtin_amdgcn_readfirstlane(last)) return;
-    double sum = lane < gridDim.x ? __builtin_bit_cast(double, atomicAdd(&left[lane], 0ull)) : 0.0;
-    sum = wave_sum_f64(sum);
-    if (lane == 0) a.loss_out[0] = (float)(a.coef / (double)a.r.groups * sum);
+    last = __builtin_amdgcn_readfirstlane(last);
+    if (last == 0) return;
+    double more = 0.0;
+    if (last == 2) {
+        more = lane < gridDim.x ? __builtin_bit_cast(double, atomicAdd(&left[lane], 0ull)) : 0.0;
+        more = wave_sum_f64(more);
+    }
+    if (lane == 0)
+        a.loss_out[0] = (float)(a.coef / (double)a.r.groups * ((double)(sum >> 2 * COUNT_BITS) / ONE + more));
 }
 
 template <uint32_t JT, uint32_t JOIN_COLS>
@@ -294,10 +318,10 @@ __global__ __launch_bounds__(JT) void k_balance_join(BalanceArgs a) {
         if (blockIdx.x % a.col_blocks == 0) a.rows_out[g] = (int32_t)n;
         if (gridDim.x == 1)
             a.loss_out[0] = (float)(a.coef * loss);
-        else if (!a.done)
+        else if (!a.total)
             a.gloss[blockIdx.x] = loss;
     }
-    if (a.done && threadIdx.x < 64) add_losses(a, loss);
+    if (a.total && threadIdx.x < 64) add_losses(a, loss);
 }
 
 // The mean over groups, from n parts of their losses: a launch's 4.4 us.
@@ -454,7 +478,7 @@ BalanceArgs balance_args(const Matrix &m, const Routes &r, float coef, const Sha
 }  // namespace
 
 // Results are kept per block where groups have several (at most MAX_PARTS
-// blocks then), and losses per group or per joining block, behind a count.
+// blocks then), and losses per group or per joining block, behind their sum.
 size_t balance_ws_bytes(uint64_t rows, uint64_t experts) {
     const uint64_t joining = MAX_PARTS / 2 * ((experts + JOIN_COLS - 1) / JOIN_COLS);
     return 8 + 8 * std::max<uint64_t>(rows, joining) + MAX_PARTS * (8 * experts + 4);
@@ -476,7 +500,7 @@ hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, 
     const bool one = r.groups == 1 && m.cols <= ONE_JOIN_COLS && sh.parts <= 256;
     a.col_blocks = one ? 1 : (m.cols + JOIN_COLS - 1) / JOIN_COLS;
     const uint32_t losses = sh.parts > 1 ? r.groups * a.col_blocks : r.groups;
-    a.done = sh.parts > 1 && losses > 1 && losses <= MAX_ADDING ? (uint32_t *)ws : nullptr;
+    a.total = sh.parts > 1 && losses > 1 && losses <= MAX_ADDING ? (unsigned long long *)ws : nullptr;
     a.partial = (uint2 *)(a.gloss + losses);
     a.prows = (uint32_t *)(a.partial + blocks * m.cols);
     a.counts_out = counts_out;
@@ -494,7 +518,7 @@ hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, 
             k_balance_join<512, JOIN_COLS><<<losses, 512, 0, s>>>(a);
         trace_mark(s, "k_balance_join");
     }
-    if (losses != 1 && !a.done) {
+    if (losses != 1 && !a.total) {
         k_balance_mean<<<1, BT, 0, s>>>(a, losses);
         trace_mark(s, "k_balance_mean");
     }
