@@ -132,14 +132,15 @@ __device__ __forceinline__ double group_factor(const BalanceArgs &a, uint32_t n)
 // Sums and counts of a block's rows.  Bound by memory where rows are many: 131072
 // x 256 fp32: 27 us, 5.1 TB/s; the vector instructions alone take 14.  Else by
 // latency (load, softmax, counts in turn): 16384 x 64 bfloat16: 5.3 us.
-// A lane adds FOLD rows in 32 bits, and what these give in 64: blocks of groups
-// that are many and long have thousands of rows a lane.
+// A lane adds up to FOLD rows in 32 bits; in blocks with more rows a lane (DEEP:
+// of groups that are many and long) what each FOLD of them give is added in 64.
 constexpr uint32_t FOLD = 64;
-template <uint32_t TYPE, uint32_t LANES, uint32_t NI>
+template <uint32_t TYPE, uint32_t LANES, uint32_t NI, bool DEEP>
 __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
     constexpr uint32_t VEC = Num<TYPE>::VEC, N = NI * VEC, RPW = 64 / LANES, COLS = LANES * N;
     constexpr uint32_t U = ROWS_AT_ONCE<NI>;
-    __shared__ double sums[BW][COLS];
+    using Sum = std::conditional_t<DEEP, double, float>;
+    __shared__ Sum sums[BW][COLS];
     __shared__ uint32_t hist[MAX_EXPERTS];
     __shared__ uint32_t rows;
     __shared__ double red[BW];
@@ -153,16 +154,14 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
     }
     float acc[N] = {};
     uint32_t n = 0, added = 0;
-    bool folded = false;
-    const auto fold = [&] {  // the wave's rows; its own lanes' sums
+    const auto fold = [&](bool first) {  // the wave's rows; a lane's own places
 #pragma unroll
         for (uint32_t i = 0; i < N; ++i) {
             const float x = groups_sum<LANES>(acc[i]);
-            double &s = sums[w][(i / VEC * LANES + sub) * VEC + i % VEC];
-            if (lane < LANES) s = folded ? s + x : x;
+            Sum &s = sums[w][(i / VEC * LANES + sub) * VEC + i % VEC];
+            if (lane < LANES) s = first ? x : s + x;
             acc[i] = 0.f;
         }
-        folded = true;
     };
     for (uint64_t r = b.first + w * RPW + lane / LANES; r - lane / LANES < b.end; r += U * BW * RPW) {
         RowBatch<TYPE, LANES, NI, U> rows_now;
@@ -177,13 +176,12 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
 #pragma unroll
             for (uint32_t i = 0; i < N; ++i) acc[i] += x[i];
         }
-        added += U;
-        if (added == FOLD) {
-            fold();
-            added = 0;
+        if constexpr (DEEP) {
+            added += U;
+            if (added % FOLD == 0) fold(added == FOLD);
         }
     }
-    fold();
+    fold(added < FOLD);
     n = wave_sum(n);
     lds_barrier();
     if (lane == 0 && n) atomicAdd(&rows, n);
@@ -199,7 +197,7 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
     const double inv = rows ? 1.0 / rows : 0.0;
     double loss = 0.0;
     for (uint32_t e = threadIdx.x; e < E; e += BT) {
-        double s = sums[0][e];
+        Sum s = sums[0][e];
 #pragma unroll
         for (uint32_t i = 1; i < BW; ++i) s += sums[i][e];
         if (a.parts > 1) {
@@ -415,8 +413,10 @@ template <uint32_t TYPE, bool GRAD, uint32_t LANES, uint32_t NI>
 void rows_kernel(const BalanceArgs &a, uint32_t grid, hipStream_t s) {
     if constexpr (GRAD)
         k_balance_grad<TYPE, LANES, NI><<<grid, BT, 0, s>>>(a);
+    else if (a.part_rows > FOLD * BW * (64 / LANES))
+        k_balance_rows<TYPE, LANES, NI, true><<<grid, BT, 0, s>>>(a);
     else
-        k_balance_rows<TYPE, LANES, NI><<<grid, BT, 0, s>>>(a);
+        k_balance_rows<TYPE, LANES, NI, false><<<grid, BT, 0, s>>>(a);
     trace_mark(s, GRAD ? "k_balance_grad" : "k_balance_rows");
 }
 
