@@ -29,7 +29,7 @@ from paper_2102_03112_amd import losses as L  # noqa: E402
 
 
 class Distill(torch.autograd.Function):
-    """sum over rows of weight * KL(teacher || student)"""
+    """Per row, weight * KL(teacher || student)"""
 
     @staticmethod
     def forward(ctx, logits, teacher, temperature, weight):

@@ -355,3 +355,45 @@ def test_distill_gradients_of_a_tail_far_from_the_kept_logits(cols, gap, weight,
     w = torch.zeros(130)
     w[:4] = weight
     check_step(z, idx, val, rest, 1.0, 130.0, w)
+
+
+@pytest.mark.parametrize("dtype", R.TYPES)
+@pytest.mark.parametrize("t", [0.05, 0.3, 10.0, 50.0])
+@pytest.mark.parametrize("rows,cols,k", [(3, 3000, 30), (130, 20_000, 64), (3, 40_000, 200)])
+def test_distill_temperatures(rows, cols, k, t, dtype):
+    log("temperatures", rows, cols, k, t, dtype)
+    z, idx, val, rest = R.student(rows, cols, k, dtype, 397, t)
+    weight = torch.zeros(rows)
+    weight[:3] = t * t
+    check_step(z, idx, val, rest, t, 40.0, weight)
+
+
+@pytest.mark.parametrize("dtype", R.TYPES)
+@pytest.mark.parametrize("t", [0.05, 0.3, 10.0, 50.0])
+@pytest.mark.parametrize("cols,k", [(3000, 30), (70_001, 200), (140_000, 256)])
+def test_top_temperatures(cols, k, t, dtype):
+    log("top temperatures", cols, k, t, dtype)
+    gen = torch.Generator().manual_seed(401)
+    check_top((3.0 * torch.randn(3, cols, generator=gen)).to(dtype).cuda(), k, t)
+
+
+@pytest.mark.parametrize("dtype", R.TYPES)
+@pytest.mark.parametrize("cols,k", [(50_001, 1024), (150_000, 700), (262_143, 1024)])
+def test_distill_long_rows_of_many_entries(cols, k, dtype):
+    """Rows of one block that take several rounds beyond its registers, with as many entries as a row may have."""
+    log("long rows, many entries", cols, k, dtype)
+    z, idx, val, rest = R.student(128, cols, k, dtype, 409)
+    weight = torch.zeros(128)
+    weight[[0, 1, 127]] = 1.0
+    check_step(z, idx, val, rest, 1.0, 40.0, weight)
+
+
+@pytest.mark.parametrize("k", [257, 1000])
+def test_distill_short_rows_of_many_entries(k):
+    """More entries than a wave, or than a block has threads, at every size of block."""
+    for cols in (1001, 2500, 5000, 9000, 20_000, 40_000):
+        log("many entries", cols, k)
+        z, idx, val, rest = R.student(128, cols, k, BF16, 419)
+        weight = torch.zeros(128)
+        weight[:3] = 1.0
+        check_step(z, idx, val, rest, 1.0, 40.0, weight)
