@@ -156,12 +156,16 @@ __global__ __launch_bounds__(BT) void k_balance_rows(BalanceArgs a) {
     uint32_t n = 0, added = 0;
     const auto fold = [&](bool first) {  // the wave's rows; a lane's own places
 #pragma unroll
-        for (uint32_t i = 0; i < N; ++i) {
-            const float x = groups_sum<LANES>(acc[i]);
-            Sum &s = sums[w][(i / VEC * LANES + sub) * VEC + i % VEC];
-            if (lane < LANES) s = first ? x : s + x;
-            acc[i] = 0.f;
+        for (uint32_t i = 0; i < N; ++i) acc[i] = groups_sum<LANES>(acc[i]);
+        if (lane < LANES) {
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i) {
+                Sum &s = sums[w][(i / VEC * LANES + sub) * VEC + i % VEC];
+                s = first ? acc[i] : s + acc[i];
+            }
         }
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) acc[i] = 0.f;
     };
     for (uint64_t r = b.first + w * RPW + lane / LANES; r - lane / LANES < b.end; r += U * BW * RPW) {
         RowBatch<TYPE, LANES, NI, U> rows_now;
