@@ -483,9 +483,10 @@ BalanceArgs balance_args(const Matrix &m, const Routes &r, float coef, const Sha
 
 // Results are kept per block where groups have several (at most MAX_PARTS
 // blocks then), and losses per group or per joining block, behind their sum.
+constexpr uint64_t LINE = 128;  // of the cache: a joining block's 16 columns are one, if they start one
 size_t balance_ws_bytes(uint64_t rows, uint64_t experts) {
     const uint64_t joining = MAX_PARTS / 2 * ((experts + JOIN_COLS - 1) / JOIN_COLS);
-    return 8 + 8 * std::max<uint64_t>(rows, joining) + MAX_PARTS * (8 * experts + 4);
+    return 2 * LINE + 8 * std::max<uint64_t>(rows, joining) + MAX_PARTS * (8 * experts + 4);
 }
 
 uint64_t balance_threads(const Matrix &m, const Routes &r) {
@@ -500,12 +501,12 @@ hipError_t launch_balance_forward(const Matrix &m, const Routes &r, float coef, 
     const Shape sh = plan_rows(m.rows, m.cols, m.type, r.group_rows, false);
     BalanceArgs a = balance_args(m, r, coef, sh);
     const uint64_t blocks = (uint64_t)r.groups * sh.parts;
-    a.gloss = (double *)(ws + 8);
+    a.gloss = (double *)(ws + LINE);
     const bool one = r.groups == 1 && m.cols <= ONE_JOIN_COLS && sh.parts <= 256;
     a.col_blocks = one ? 1 : (m.cols + JOIN_COLS - 1) / JOIN_COLS;
     const uint32_t losses = sh.parts > 1 ? r.groups * a.col_blocks : r.groups;
     a.total = sh.parts > 1 && losses > 1 && losses <= MAX_ADDING ? (unsigned long long *)ws : nullptr;
-    a.partial = (uint2 *)(a.gloss + losses);
+    a.partial = (uint2 *)(ws + LINE + (8ull * losses + LINE - 1) / LINE * LINE);
     a.prows = (uint32_t *)(a.partial + blocks * m.cols);
     a.counts_out = counts_out;
     a.rows_out = rows_out;
