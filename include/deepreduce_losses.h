@@ -19,8 +19,9 @@
  * capture would refuse.  Results do not depend on the order in which blocks
  * run: the same inputs give the same bits.
  *
- * A launch counts its threads in 32 bits: rows x cols that would need more
- * (some 10^11 numbers, or 10^7 groups of a balance loss) are EINVAL.
+ * A launch counts its threads in 32 bits: calls that would need more are
+ * EINVAL (some 10^11 numbers; 2^24 rows of a distillation, however short, 2^23
+ * to 2^25 of dr_top_logits, 2^24 groups of a balance loss).
  *
  * Logits.  A matrix of rows x cols numbers of one type, each row contiguous,
  * rows `row_stride` numbers apart; any alignment that suits the type.  -inf

@@ -216,7 +216,7 @@ __device__ __forceinline__ float entry_p(float y, float inv_t, float m_p, float 
 }
 
 // One wave per row joins its slices; NK entries per lane.  Bound by latency (an
-// index, then the logit it names): 6.5 us for 1500 rows of 100 entries, 3.7 for 16.
+// index, then the logit it names): 6.6 us for 1500 rows of 100 entries, 3.8 for 16.
 template <uint32_t TYPE, int NK>
 __global__ __launch_bounds__(DIST_THREADS) void k_distill_join(DistillArgs a) {
     const uint32_t lane = threadIdx.x & 63u;
@@ -345,14 +345,15 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
 // A step (GRAD), or the forward pass of a row that THREADS threads hold, of one
 // row by one block.  A step's first RES vectors of every thread stay in
 // registers from the sum to the gradient.  What a longer row has beyond
-// them is read twice, MORE vectors at a time, the second time from the cache
-// beside the memory: 256 CUs hold at most 512 rows at a time, 128 MiB of 131072
-// 16-bit numbers, and it holds 256.  A CU's blocks are rarely in one phase, so
-// that one loads and stores while another adds.  The sum is relative to the
-// largest kept logit, which is known before the row has arrived.  Bound by
-// memory: 4096 x 131072 bfloat16: 405 us, 5.1 TB/s of the logits' and the
-// gradient's bytes; the vector instructions alone take 171.  Short rows by their
-// latency: 256 x 32000 fp32, one row per CU: 15.5 us.
+// them is read twice, MORE vectors at a time, the second time mostly from L2:
+// blocks of 1024 threads have a CU each, and the second halves of the 32 rows of
+// 131072 16-bit numbers that an XCD's CUs then hold are the 4 MiB of its L2
+// (1.11 GB are read beyond it of the 1.01 that have to be, with 0.50 read
+// twice).  The sum is relative to the largest kept logit, which is known before
+// the row has arrived.  Bound by memory: 4096 x 131072 bfloat16: 403 us, 5.2
+// TB/s of the logits' and the gradient's bytes (in a profiler's trace 407 at
+// least and 436 on average); the vector instructions alone take 173.  Short rows
+// by their latency: 256 x 32000 fp32, one row per CU: 16 us.
 constexpr int RES = 8;
 
 // Adds a run's numbers but for the kept columns, relative to a reference, and
@@ -398,6 +399,9 @@ __device__ __forceinline__ void grad_run(Vec<TYPE> (&v)[NV], typename Num<TYPE>:
     }
 }
 
+// The bounds on waves per SIMD: a step's short rows spill ten registers at eight
+// (16000 x 4000 bfloat16: 80 us, 70 at seven); 512 threads, of which three blocks
+// share a CU, spill two of 16-bit rows.
 template <uint32_t TYPE, uint32_t THREADS, bool GRAD>
 __global__ __launch_bounds__(THREADS, !GRAD ? 8 : THREADS < 512 ? 7 : 6) void k_distill_row(DistillArgs a) {
     using N = Num<TYPE>;
@@ -575,7 +579,7 @@ void grad_kernel(const DistillArgs &a, hipStream_t s) {
 // Whether a step takes its rows one by one: where they are many, or so short
 // that a block is through with one as soon as it would be with a slice; and a
 // row's bitmap must fit beside its entries.  131072 bfloat16 columns, one by
-// one and by slices: 64 rows 18 and 14 us, 128 rows 20 and 21, 256 rows 29 and
+// one and by slices: 64 rows 18 and 15 us, 128 rows 20 and 21, 256 rows 29 and
 // 40; 32 rows of 32000: 9.6 and 10.5.
 constexpr uint32_t ROW_MAX_COLS = 1u << 18;
 constexpr uint64_t row_bytes(uint32_t cols, uint32_t type) { return (uint64_t)cols * type_bytes(type); }
@@ -584,7 +588,7 @@ bool step_by_rows(const Matrix &m) {
 }
 // A forward pass gains by rows of up to 256 threads' registers, being one
 // launch (4000 rows of 8000 bfloat16 columns: 20 us one by one, 24 by slices;
-// of 32000: 55 and 53).
+// of 32000: 55 and 53, all on logits in the cache).
 constexpr bool forward_by_rows(uint32_t cols, uint32_t type) { return row_bytes(cols, type) <= 256 * RES * 16; }
 static_assert(!forward_by_rows(1u << 30, TYPE_F32) && !forward_by_rows((1u << 30) + 8192, TYPE_F32) &&
                   !forward_by_rows(1u << 30, TYPE_BF16) && !forward_by_rows(0x7fffffffu, TYPE_F16) &&
@@ -596,9 +600,9 @@ static_assert(ROW_MAX_COLS <= 64 * 1024 * 4 && 16384 <= 64 * 256 * 4, "longest s
 
 // Threads per row: as many as hold it in RES vectors each, but 512 up to twice
 // that, where three blocks share a CU and one of 1024 threads would have it for
-// itself (2048 x 65536 bfloat16: 100 us, and 122 with 1024).  At 256, 512 and
-// 1024 threads, 4096 x 131072 takes 494, 420 and 410 us; at 64, 128 and 256,
-// 30000 x 2000 takes 62, 85 and 110.
+// itself (2048 x 65536 bfloat16: 103 us, and 122 with 1024).  At 256, 512 and
+// 1024 threads, 4096 x 131072 takes 494, 420 and 403 us; at 64, 128 and 256,
+// 30000 x 2000 takes 68, 86 and 117.
 uint32_t row_threads(const Matrix &m) {
     const uint32_t vec = 16 / type_bytes(m.type), vecs = (m.cols + vec - 1) / vec;
     for (uint32_t t = 64; t <= 256; t *= 2)
