@@ -136,6 +136,15 @@ __device__ __forceinline__ float rescale(float x, float a, float b, float c) {
     return x == 0.f ? 0.f : x * exp2_fast((a - b) * c);
 }
 
+// A largest logit over the temperature, as a finite float (-inf of none).
+__device__ __forceinline__ float quotient(float y0, float inv_t) {
+    return y0 == F_NEG_INF ? y0 : fminf(fmaxf(y0 * inv_t, F_LOWEST), -F_LOWEST);
+}
+// A teacher's reference from which on its rounding to a float is more than an
+// exponent takes: the quotient is the float itself then, and entries are
+// compared with the largest one before they are divided.
+constexpr float FAR_REFERENCE = 16777216.f;
+
 // A row's result from its columns not kept (m_tail, tail: a reference at least
 // near their maximum, and their sum relative to it) and its kept entries:
 // entry(i, x, y) gives the lane's i-th of n, the student's logit x and the
@@ -176,8 +185,8 @@ __device__ __forceinline__ RowResult row_result(float m_tail, double tail, uint3
     sum_p = wave_sum_f64(sum_p);
     sum_d = wave_sum_f64(sum_d);
     // The teacher's reference: the largest logit over the temperature, or rest.
-    const double y0_t = y0 == F_NEG_INF ? (double)y0 : fmin(fmax((double)y0 * inv_t, (double)F_LOWEST), -(double)F_LOWEST);
-    const float m_p = fmaxf((float)y0_t, rest);
+    const float y0_f = quotient(y0, inv_t), m_p = fmaxf(y0_f, rest);
+    const double y0_t = fabsf(m_p) < FAR_REFERENCE ? (double)y0 * (double)inv_t : (double)y0_f;
     const float y0_p = y0 == F_NEG_INF ? 0.f : exp_below((float)(y0_t - m_p));  // and now relative to m_p
     sum_d = y0_p > 0.f ? y0_p * (sum_d + (y0_t - m_p) * sum_p) : 0.0;
     sum_p *= y0_p;
@@ -207,12 +216,13 @@ __device__ __forceinline__ RowResult row_result(float m_tail, double tail, uint3
     return r;
 }
 
-// p of an entry with the teacher's logit y, from the saved reference and 1 /
-// sum.  A quotient below a float's range counts as the range's end, also where
-// that is the reference.
-__device__ __forceinline__ float entry_p(float y, float inv_t, float m_p, float inv_sum) {
+// p of an entry with the teacher's logit y of a row whose largest is y0 (read
+// where the reference is far alone), from the saved numbers.
+__device__ __forceinline__ float entry_p(float y, float y0, float inv_t, float c, const float *stats) {
     if (y == F_NEG_INF) return 0.f;
-    return exp_below(m_p == F_LOWEST ? fmaxf(y * inv_t, F_LOWEST) - m_p : fmaf(y, inv_t, -m_p)) * inv_sum;
+    const float m_p = stats[4];
+    if (fabsf(m_p) < FAR_REFERENCE) return exp_below(fmaf(y, inv_t, -m_p)) * stats[5];
+    return exp2_fast((y - y0) * c) * exp_below(quotient(y0, inv_t) - m_p) * stats[5];
 }
 
 // One wave per row joins its slices; NK entries per lane.  Bound by latency (an
@@ -280,6 +290,7 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
     using N = Num<TYPE>;
     using T = typename N::T;
     constexpr uint32_t VEC = N::VEC, PER = MAX_TEACHER / DIST_THREADS;
+    __shared__ float red[DIST_THREADS / 64];
     const uint64_t row = blockIdx.x / a.sl.n;
     const uint32_t s = blockIdx.x % a.sl.n, start = s * a.sl.len, n = min(a.sl.len, a.m.cols - start);
     T *out = (T *)a.grad + row * a.grad_stride + start;
@@ -301,6 +312,13 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
     const float m = st[0] == F_NEG_INF ? 0.f : st[0], m_tail = st[2] == F_NEG_INF ? 0.f : st[2];
     // no gradient where the teacher's row is no distribution
     const float scale = w * u * a.inv_t, q = st[5] > 0.f ? scale * st[1] : 0.f, f = scale * st[3];
+    float y0 = F_NEG_INF;  // the row's, of all slices
+    if (!(fabsf(st[4]) < FAR_REFERENCE)) {
+        for (uint32_t k = threadIdx.x; k < a.t.k; k += DIST_THREADS)
+            if (load_index(a.t.idx, row * a.t.idx_stride + k, a.t.idx_type, a.m.cols) < a.m.cols)
+                y0 = fmaxf(y0, load_num(a.t.val, row * a.t.val_stride + k, a.t.val_type));
+        y0 = block_max_f<DIST_THREADS>(y0, red);
+    }
     // the kept columns of this slice: read before any thread writes, written after all have
     uint32_t at[PER];
     float g[PER];
@@ -313,7 +331,7 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
         if (j >= n) continue;
         const float x = num_float<TYPE>(p[j]), y = load_num(a.t.val, row * a.t.val_stride + k, a.t.val_type);
         at[i] = j;
-        g[i] = q * exp2_fast((x - m) * a.c) - scale * entry_p(y, a.inv_t, st[4], st[5]);
+        g[i] = q * exp2_fast((x - m) * a.c) - scale * entry_p(y, y0, a.inv_t, a.c, st);
     }
     __syncthreads();
     const Base2 to2(m_tail, a.c);
@@ -516,10 +534,16 @@ __global__ __launch_bounds__(THREADS, !GRAD ? 8 : THREADS < 512 ? 7 : 6) void k_
             grad_run<TYPE, THREADS>(u, out + e0, n - e0, to2, f2);
         }
     }
+    float y0 = F_NEG_INF;
+    if (!(fabsf(row_stats[4]) < FAR_REFERENCE)) {
+        for (uint32_t k = threadIdx.x; k < a.t.k; k += THREADS)
+            if (ej[k] < n) y0 = fmaxf(y0, ey[k]);
+        y0 = block_max_f<THREADS>(y0, red[0]);
+    }
     __syncthreads();  // the kept columns are written again
     for (uint32_t k = threadIdx.x; k < a.t.k; k += THREADS) {
         if (ej[k] >= n) continue;
-        const float p_k = entry_p(ey[k], a.inv_t, row_stats[4], row_stats[5]);
+        const float p_k = entry_p(ey[k], y0, a.inv_t, a.c, row_stats);
         out[ej[k]] = num_round<TYPE>(q * exp2_fast((ex[k] - m) * a.c) - scale * p_k);
     }
 }

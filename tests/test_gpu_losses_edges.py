@@ -397,3 +397,28 @@ def test_distill_short_rows_of_many_entries(k):
         weight = torch.zeros(128)
         weight[:3] = 1.0
         check_step(z, idx, val, rest, 1.0, 40.0, weight)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("values", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(8, 700), (8, 40_000), (130, 20_000)])
+def test_distill_of_large_teachers(rows, cols, values, dtype):
+    """Teachers' logits of any size, over temperatures whose quotients a float rounds by more than an exponent takes:
+    whole rows of one number, one that stands out, two near each other."""
+    log("large teachers", rows, cols, values, dtype)
+    near = 1.0 - 2.0 ** -8
+    for t in (0.7, 1.0, 1.5, 3.0, 50.0):
+        for size in (2e7, 3e9, 3e20, 1e37, torch.finfo(values).max):
+            z, idx, val, rest = R.student(rows, cols, 20, dtype, 421, t)
+            val[0], val[1] = -size, size
+            val[2, :], val[2, 3] = -size, -size * near
+            val[3, :], val[3, 5] = size * near, size
+            val[4, 1:] = -size
+            val[5, 1:] = -size
+            val[6] = -size
+            val[7, 7], val[7, 8] = 1e9, 1e9
+            rest[:4] = -math.inf
+            rest[5] = -math.inf
+            weight = torch.zeros(rows)
+            weight[:8] = 1.0
+            check_step(z, idx, val.to(values), rest, t, 40.0, weight)
