@@ -336,13 +336,13 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
     __syncthreads();
     const Base2 to2(m_tail, a.c);
     const float f2 = f * to2.to(m_tail);
-    const bool low = fabsf(m_tail * a.c) >= 1e30f;  // all near the lowest number
+    const bool far = !(fabsf(m_tail * a.c) < BASE2_FAR);  // a mask's numbers, say: from x - m_tail
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const uint32_t s0 = i * DIST_THREADS * VEC, e0 = s0 + threadIdx.x * VEC;
         if (s0 >= n) break;
         float x[VEC];
-        if (low) {
+        if (far) {
 #pragma unroll
             for (uint32_t e = 0; e < VEC; ++e) x[e] = f * exp2_fast((v[i].get(e) - m_tail) * a.c);
         } else {
@@ -516,7 +516,7 @@ __global__ __launch_bounds__(THREADS, !GRAD ? 8 : THREADS < 512 ? 7 : 6) void k_
     const float r = to2.r, f = scale * row_stats[3];
     to2.r += (float)size;
     const float f2 = ldexpf(f * Base2(ref, a.c).to(ref), (int)(to2.r - r) - size);
-    if (fabsf(ref * a.c) >= 1e30f) {  // all near the lowest number
+    if (!(fabsf(ref * a.c) < BASE2_FAR)) {  // a mask's numbers, say: from x - ref
 #pragma unroll 1
         for (uint32_t e0 = threadIdx.x * VEC; e0 < n; e0 += STEP) {
             const Vec<TYPE> u = load_vec<TYPE, false>(p, e0, n, avail);

@@ -333,14 +333,16 @@ __device__ __forceinline__ float exp_below(float x) { return exp2_fast(x * LOG2E
 
 // exp((x - m) / t) as 2^(x c - R) times 2^(R - m c), c = log2(e) / t and R the
 // whole number next to m c: one fused operation per number, whose only
-// rounding is that of a small result, and the second factor once.  R = 0 where
-// m c is no ordinary number; such sums come out of range and are formed again
-// from x - m.
+// rounding is that of a small result, and the second factor once.  Where m c is
+// so large that a float's whole numbers are too far apart (from BASE2_FAR on
+// R - m c would be beyond 4, and beyond all exponents soon), R = 0: such sums come
+// out of range and are formed again from x - m.
+constexpr float BASE2_FAR = 1e8f;
 struct Base2 {
     float c, r;
     __device__ __forceinline__ Base2(float m, float c_) : c(c_) {
         const float x = rintf(m * c_);
-        r = fabsf(x) < 1e30f ? x : 0.f;
+        r = fabsf(x) < BASE2_FAR ? x : 0.f;
     }
     __device__ __forceinline__ float operator()(float x) const { return exp2_fast(fmaf(x, c, -r)); }
     __device__ __forceinline__ float to(float m) const { return exp2_fast(-fmaf(m, c, -r)); }

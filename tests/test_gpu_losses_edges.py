@@ -422,3 +422,45 @@ def test_distill_of_large_teachers(rows, cols, values, dtype):
             weight = torch.zeros(rows)
             weight[:8] = 1.0
             check_step(z, idx, val.to(values), rest, t, 40.0, weight)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(8, 700), (8, 40_000), (130, 20_000)])
+def test_distill_of_students_of_every_size(rows, cols, dtype):
+    """Student's logits of any size: whole rows, whole tails and single columns masked with a large number, tails and
+    kept columns that differ little beside it."""
+    log("large students", rows, cols, dtype)
+    near = 1.0 - 2.0 ** -8
+    for t in (0.7, 1.0, 3.0):
+        for size in (1e6, 7e7, 2e8, 1e9, 3e9, 1e10, 1e12, 3e20, 1e29, 2e30, 1e37):
+            z, idx, val, rest = R.student(rows, cols, 20, dtype, 431, t)
+            kept = torch.zeros(rows, cols, dtype=torch.bool).scatter_(1, idx.long(), True)
+            third = torch.arange(cols) % 3 == 0
+            f = z.float()
+            f[0] = -size
+            f[1] = torch.where(kept[1], f[1], -size)
+            f[2] = torch.where(kept[2], f[2], torch.where(third, -size, -size * near))
+            f[3] = torch.where(kept[3], -size, f[3])
+            f[4] = torch.where(third, -size * near, -size)
+            f[5] = size
+            f[6] = torch.where(third & ~kept[6], -size, f[6])
+            f[7] = torch.where(kept[7], f[7], torch.where(third, size, size * near))
+            rest[[0, 1]] = -math.inf
+            weight = torch.zeros(rows)
+            weight[:8] = 1.0
+            check_step(f.to(dtype), idx, val, rest, t, 40.0, weight)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols,k", [(60, 8), (9000, 64), (140_000, 100)])
+def test_top_logits_of_every_size(cols, k, dtype):
+    log("top of every size", cols, k, dtype)
+    third = torch.arange(cols) % 3 == 0
+    gen = torch.Generator().manual_seed(433)
+    x = torch.randn(1, cols, generator=gen)[0]
+    for t in (0.7, 1.0, 3.0):
+        for size in (1e6, 7e7, 2e8, 1e9, 3e9, 1e10, 1e12, 3e20, 1e29, 2e30, 1e37):
+            near = size * (1.0 - 2.0 ** -8)
+            rows = [torch.full((cols,), -size), torch.full((cols,), size), torch.where(third, size, near),
+                    torch.where(third, -size, -near), torch.where(third, -size, x), torch.where(third, size, x)]
+            check_top(torch.stack(rows).to(dtype).cuda(), k, t)
