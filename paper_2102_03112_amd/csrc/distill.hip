@@ -112,6 +112,7 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_slice(DistillArgs a) {
         v[i].keep_packed();
         most.add(v[i]);
     }
+    most.complete(v);
     const float mx = block_max_f<DIST_THREADS>(most.value(), red[0]);
     const Base2 to2(mx, a.c);
     float sum = 0.f;
@@ -475,6 +476,7 @@ __global__ __launch_bounds__(THREADS, !GRAD ? 8 : THREADS < 512 ? 7 : 6) void k_
     }
     sum = block_sum_f<THREADS>(sum, red[1]);
     if (!GRAD) {  // the saved numbers are relative to the largest logit not kept
+        most.complete(v);
         const float mx = block_max_f<THREADS>(most.value(), red[0]);
         ref = mx > F_NEG_INF ? mx : ref;
     }

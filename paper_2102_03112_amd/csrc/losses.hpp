@@ -177,16 +177,15 @@ struct Vec {
 };
 
 // The largest number of some vectors, kept as bits (-inf of none).  32-bit
-// numbers: a float.  float16: two halves.  bfloat16: two halves of each of two
-// kinds, as whole numbers: the largest of the bits with their sign, which is
-// the maximum unless all are negative, and the smallest without, which is the
-// maximum then.  (Read as float16, bfloat16 numbers from 2^121 on would be NaN,
-// and the maximum of such halves no number of the vectors.)
+// numbers: a float.  float16: two halves.  bfloat16: two halves as whole numbers,
+// the largest of the bits with their sign; where a half of all vectors is
+// negative, the smallest bits without it are the maximum, for which complete()
+// goes over the vectors again.  (Read as float16, bfloat16 numbers from 2^121 on
+// would be NaN, and the maximum of such halves no number of the vectors.)
 template <uint32_t TYPE>
 struct Largest {
     using N = Num<TYPE>;
     uint32_t w = TYPE == TYPE_F32 ? N::NEG_INF : N::NEG_INF * 0x10001u;
-    uint32_t low = N::NEG_INF * 0x10001u;  // bfloat16 only
 
     __device__ __forceinline__ void add(const Vec<TYPE> &v) {
         if constexpr (TYPE == TYPE_F32) {
@@ -195,10 +194,23 @@ struct Largest {
         } else if constexpr (TYPE == TYPE_BF16) {
             w = max_halves_signed(max_halves_signed(w, v.w[0]),
                                   max_halves_signed(max_halves_signed(v.w[1], v.w[2]), v.w[3]));
-            low = min_halves_unsigned(min_halves_unsigned(low, v.w[0]),
-                                      min_halves_unsigned(min_halves_unsigned(v.w[1], v.w[2]), v.w[3]));
         } else {
             w = max_halves(max_halves(w, v.w[0]), max_halves(max_halves(v.w[1], v.w[2]), v.w[3]));
+        }
+    }
+    // after all of v, and no others, were added
+    template <int NV>
+    __device__ __forceinline__ void complete(const Vec<TYPE> (&v)[NV]) {
+        if constexpr (TYPE == TYPE_BF16) {
+            if (w & 0x80008000u) {
+                uint32_t low = N::NEG_INF * 0x10001u;
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    low = min_halves_unsigned(
+                        min_halves_unsigned(low, v[i].w[0]),
+                        min_halves_unsigned(min_halves_unsigned(v[i].w[1], v[i].w[2]), v[i].w[3]));
+                w = (w & 0x8000u ? low & 0xffffu : w & 0xffffu) | (w >> 31 ? low & 0xffff0000u : w & 0xffff0000u);
+            }
         }
     }
     __device__ __forceinline__ float value() const {
@@ -206,12 +218,7 @@ struct Largest {
         if constexpr (TYPE == TYPE_F32) {
             return __uint_as_float(w);
         } else {
-            uint32_t a = w & 0xffffu, b = w >> 16;
-            if constexpr (TYPE == TYPE_BF16) {
-                a = a & 0x8000u ? low & 0xffffu : a;
-                b = b & 0x8000u ? low >> 16 : b;
-            }
-            const float x = num_float<TYPE>((T)a), y = num_float<TYPE>((T)b);
+            const float x = num_float<TYPE>((T)w), y = num_float<TYPE>((T)(w >> 16));
             return x > y ? x : y;
         }
     }

@@ -310,6 +310,7 @@ __global__ __launch_bounds__(NT) void k_top_slice(TopArgs a) {
     Largest<TYPE> most;
 #pragma unroll
     for (int i = 0; i < NV; ++i) most.add(v[i]);
+    most.complete(v);
     // every wave's nth largest, then the largest of them that K threads reach
     const uint32_t key16 = order_key(most.value()) >> 16;
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u;
