@@ -131,7 +131,7 @@ __device__ __forceinline__ double group_factor(const BalanceArgs &a, uint32_t n)
 
 // Sums and counts of a block's rows.  Bound by memory where rows are many: 131072
 // x 256 fp32: 27 us, 5.1 TB/s; the vector instructions alone take 14.  Else by
-// latency (load, softmax, counts in turn): 16384 x 64 bfloat16: 5.4 us.
+// latency (load, softmax, counts in turn): 16384 x 64 bfloat16: 5.3 us.
 // A lane adds up to FOLD rows in 32 bits; in blocks with more rows a lane (DEEP:
 // of groups that are many and long) what each FOLD of them give is added in 64.
 constexpr uint32_t FOLD = 64;

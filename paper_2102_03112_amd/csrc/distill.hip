@@ -227,7 +227,7 @@ __device__ __forceinline__ float entry_p(float y, float y0, float inv_t, float c
 }
 
 // One wave per row joins its slices; NK entries per lane.  Bound by latency (an
-// index, then the logit it names): 6.6 us for 1500 rows of 100 entries, 3.8 for 16.
+// index, then the logit it names): 6.5 us for 1500 rows of 100 entries, 3.8 for 16.
 template <uint32_t TYPE, int NK>
 __global__ __launch_bounds__(DIST_THREADS) void k_distill_join(DistillArgs a) {
     const uint32_t lane = threadIdx.x & 63u;
@@ -370,8 +370,8 @@ __global__ __launch_bounds__(DIST_THREADS) void k_distill_grad(DistillArgs a) {
 // (1.11 GB are read beyond it of the 1.01 that have to be, with 0.50 read
 // twice).  The sum is relative to the largest kept logit, which is known before
 // the row has arrived.  Bound by memory: 4096 x 131072 bfloat16: 403 us, 5.2
-// TB/s of the logits' and the gradient's bytes (in a profiler's trace 407 at
-// least and 436 on average); the vector instructions alone take 173.  Short rows
+// TB/s of the logits' and the gradient's bytes (in a profiler's trace 415 at
+// least and 435 on average); the vector instructions alone take 173.  Short rows
 // by their latency: 256 x 32000 fp32, one row per CU: 16 us.
 constexpr int RES = 8;
 

@@ -289,8 +289,8 @@ __device__ __forceinline__ float2 sum_below(const SliceView<TYPE, NT> &sl, float
 // multiply-add, an exponential at half rate, add), the slice itself (bound,
 // list, ranks) some 300 instructions a wave: so slices are as long as registers
 // allow (plan_top; blocks of 256 and 1024 threads were slower for long rows).
-// Bound by vector issue beside memory: 2048 x 131072 bfloat16, K 64: 104 us, 5.2
-// TB/s, of which the vector instructions alone take 88.  777 x 50001 fp32, K 100:
+// Bound by vector issue beside memory: 2048 x 131072 bfloat16, K 64: 100 us, 5.4
+// TB/s, of which the vector instructions alone take 84.  777 x 50001 fp32, K 100:
 // 32 us, 4.9 TB/s, and 17: three blocks share a CU, and 18 of the 1554 are left to
 // a third round.  8 x 32000: 8 us, one block's latency.
 template <uint32_t TYPE, int NV, uint32_t NT>
