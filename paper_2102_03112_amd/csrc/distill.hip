@@ -637,7 +637,7 @@ uint32_t row_threads(const Matrix &m) {
 }
 // Every thread of a step, also one beyond the row, finds its bits in the bitmap.
 constexpr bool bitmap_holds_steps(uint32_t n, uint32_t threads, uint32_t vec) {
-    const uint32_t step = threads * vec, last = (n - 1) / step * (step / vec) + threads - 1;  // vector of the last thread
+    const uint32_t step = threads * vec, last = (n - 1) / step * threads + threads - 1;  // the last thread's vector
     return (last + 1) * vec <= 32 * row_bitmap_words(n, step);
 }
 static_assert(bitmap_holds_steps(1, 64, 8) && bitmap_holds_steps(512, 64, 8) && bitmap_holds_steps(513, 64, 8) &&

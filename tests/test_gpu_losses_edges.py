@@ -297,7 +297,8 @@ def test_a_workspace_of_the_longest_batch_serves_shorter_ones(dtype):
     seen = {}
     for n in (512, 511, 300, 100, 8, 1):
         zn, teacher = many[0][:n], L.Teacher(*(x[:n] for x in many[1:]))
-        loss, stats, loss2 = torch.zeros(n, device="cuda"), torch.zeros(n, L.STATS, device="cuda"), torch.zeros(n, device="cuda")
+        loss, loss2 = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+        stats = torch.zeros(n, L.STATS, device="cuda")
         grad = torch.zeros_like(zn)
         L.distill_forward(zn, teacher, 1.0, None, loss, stats, ws)
         L.distill_step(zn, teacher, 1.0, None, loss2, grad, ws)
